@@ -7,11 +7,11 @@
 
 #include <algorithm>
 #include <mutex>
-#include <vector>
 
 #include "../../include/tri.h"
 #include "host.hpp"
 #include "kernels.hpp"
+#include "stage.hpp"
 
 using namespace tri;
 
@@ -55,16 +55,7 @@ tri_status tri::check_config(const tri_layer_config* c) {
   return TRI_OK;
 }
 
-namespace {
-
-constexpr size_t kAlign = 256;
-inline size_t up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-// Projections with at most this many rows take the weight-streaming path.
-constexpr int kSkinnyMaxRows = 128;
-
-tri_status check_batch_scalars(const tri_batch* b) {
+tri_status tri::check_batch_scalars(const tri_batch* b) {
   if (!b) return TRI_ERR_NULL;
   if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_q_len < 0 || b->max_ctx_len < 0)
     return TRI_ERR_SHAPE;
@@ -74,6 +65,11 @@ tri_status check_batch_scalars(const tri_batch* b) {
   if ((int64_t)b->n_seqs > 0 && (int64_t)b->max_q_len * b->n_seqs < b->n_tokens) return TRI_ERR_SHAPE;
   return TRI_OK;
 }
+
+namespace {
+
+// Projections with at most this many rows take the weight-streaming path.
+constexpr int kSkinnyMaxRows = 128;
 
 struct Layout {
   size_t tok_slot, tok_row, rope, h, q, attn, x1, h2, act, part;
@@ -230,46 +226,6 @@ Layout layout_of(const tri_layer_config* c, const tri_batch* b) {
   return l;
 }
 
-// ------------------------------------------------------------ profiling --
-struct Profiler {
-  std::mutex mu;
-  bool on = false;
-  struct Rec { int stage; hipEvent_t a, b; };
-  std::vector<Rec> pending;
-  std::vector<hipEvent_t> pool;
-  int launches[ST_COUNT] = {};
-  double ms[ST_COUNT] = {};
-  hipEvent_t get() {
-    if (!pool.empty()) { hipEvent_t e = pool.back(); pool.pop_back(); return e; }
-    hipEvent_t e = nullptr;
-    if (hipEventCreate(&e) != hipSuccess) return nullptr;
-    return e;
-  }
-};
-Profiler& prof() { static Profiler p; return p; }
-
-// Records an event pair around one stage when profiling is on.
-struct StageTimer {
-  int stage;
-  hipStream_t s;
-  hipEvent_t a = nullptr, b = nullptr;
-  StageTimer(int st, hipStream_t str, bool timed = true) : stage(st), s(str) {
-    Profiler& p = prof();
-    if (!timed || !p.on) return;
-    std::lock_guard<std::mutex> g(p.mu);
-    a = p.get();
-    b = p.get();
-    if (a && b) hipEventRecord(a, s);
-  }
-  ~StageTimer() {
-    if (!a || !b) return;
-    Profiler& p = prof();
-    hipEventRecord(b, s);
-    std::lock_guard<std::mutex> g(p.mu);
-    p.pending.push_back({stage, a, b});
-  }
-};
-
 template <typename T>
 T* at(void* ws, size_t off) { return (T*)((char*)ws + off); }
 
@@ -330,21 +286,11 @@ bool side_ready(SideStream& x, hipStream_t caller) {
 }
 
 
-#define TRI_HIP(expr)                              \
-  do {                                             \
-    if ((expr) != hipSuccess) return TRI_ERR_HIP;  \
-  } while (0)
-
 tri_status run_linear(const void* A, int lda, const void* B, int M, int N, int K, const Epi& epi,
                       float* part, hipStream_t s) {
   if (M <= kSkinnyMaxRows) TRI_HIP(launch_skinny(A, lda, B, K, M, N, K, epi, part, s));
   else TRI_HIP(launch_gemm(A, lda, B, K, M, N, K, epi, part, s));
   return TRI_OK;
-}
-
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + nb && y < x + na;
 }
 
 // The fp32 storage mode's launch sequence (arguments already validated): the

@@ -1,6 +1,9 @@
 // Host-side definitions shared by the C-ABI sources: config validation and
 // the stage list that both the per-stage timers and the work model index.
 #pragma once
+#include <stddef.h>
+#include <stdint.h>
+
 #include "../../include/tri.h"
 
 namespace tri {
@@ -19,6 +22,16 @@ inline constexpr const char* kStageName[ST_COUNT] = {
 
 // Validates a layer config (TRI_OK, or the status the entry points return).
 tri_status check_config(const tri_layer_config* c);
+// The same for a batch's host scalars.
+tri_status check_batch_scalars(const tri_batch* b);
+
+constexpr size_t kAlign = 256;  // workspace regions
+inline size_t up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
 
 // The layer entry points' common body (tri_layer_prefill when decode is
 // false, tri_layer_decode when true) on a workspace of ws_bytes; with timed =
