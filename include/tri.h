@@ -256,6 +256,158 @@ tri_status tri_kvcache_append(const tri_layer_config* cfg, const tri_kv_cache* c
                               const tri_batch* batch, const void* k_new, const void* v_new,
                               void* stream);
 
+/* ---- operators of a long context: rotary positions of other models' kinds, a
+ * key/value cache of one byte per value, attention over it and its eviction.
+ * They take the pieces that the layer calls fuse (the serving loop around the
+ * Thinker, Section II-A, calls them between its own projections); conventions
+ * and errors as above.  At most 65535 sequences and heads a call
+ * (TRI_ERR_RANGE): they are extents of the launch grid.                       */
+
+/* Rotary positions.  Of every head's head_dim values the first rotary_dim are
+ * rotated in pairs, the rest copied:
+ *   (a, b) -> m (a cos t - b sin t, b cos t + a sin t),  t = pos * f_i
+ * for pair i < rotary_dim / 2, in double precision up to the reduced angle.
+ * Pairs: TRI_ROPE_HALF (i, i + rotary_dim/2), TRI_ROPE_INTERLEAVED (2i, 2i+1).
+ * Frequencies, w_i = base^(-2i / rotary_dim):
+ *  TRI_ROPE_PLAIN   f = w
+ *  TRI_ROPE_LINEAR  f = w / factor (positions interpolated)
+ *  TRI_ROPE_BASE    base scaled: f = (base factor^(r/(r-2)))^(-2i/r), r = rotary_dim
+ *                   (as PLAIN for r = 2)
+ *  TRI_ROPE_TURNS   by the turns n = original_len w / (2 pi) that a pair makes over
+ *                   the context it was trained on: t = clamp((n - low) / (high -
+ *                   low), 0, 1), f = w (t + (1 - t) / factor)
+ *  TRI_ROPE_INDEX   the same blend, linear in the index between the pairs that
+ *                   make `high` and `low` turns: at(n) = r ln(original_len / (2 pi
+ *                   n)) / (2 ln base), lo = max(floor(at(high)), 0), hi =
+ *                   min(ceil(at(low)), r - 1), u = clamp((i - lo) / max(hi - lo,
+ *                   0.001), 0, 1), f = w (1 - u) + (w / factor) u
+ * magnitude m scales cos and sin (1 for none).                                 */
+typedef enum { TRI_ROPE_HALF = 0, TRI_ROPE_INTERLEAVED = 1 } tri_rope_layout;
+typedef enum {
+  TRI_ROPE_PLAIN = 0,
+  TRI_ROPE_LINEAR = 1,
+  TRI_ROPE_BASE = 2,
+  TRI_ROPE_TURNS = 3,
+  TRI_ROPE_INDEX = 4
+} tri_rope_scaling;
+typedef struct {
+  int32_t head_dim;     /* 2 .. 256, even                                         */
+  int32_t rotary_dim;   /* 2 .. head_dim, even                                    */
+  int32_t layout;       /* tri_rope_layout                                        */
+  int32_t scaling;      /* tri_rope_scaling                                       */
+  int32_t original_len; /* TURNS, INDEX: the trained context (> 0)                */
+  float base;           /* > 0; INDEX: > 1                                        */
+  float factor;         /* > 0 (every kind but PLAIN)                             */
+  float low, high;      /* TURNS, INDEX: 0 < low < high                           */
+  float magnitude;      /* finite                                                 */
+} tri_rope_config;
+
+/* y = x rotated.  x and y: device [n_tokens][n_heads][head_dim] of dtype (bf16 or
+ * float32), tokens x_stride and y_stride elements apart (>= n_heads * head_dim:
+ * the q and k heads of fused projection rows are one call); aligned to an
+ * element, fastest where addresses and strides are multiples of 16 bytes and
+ * rotary_dim of 32 bytes.  y may be x itself (same stride); any other overlap is
+ * TRI_ERR_ALIAS.  pos: device int32 [n_tokens], any sign.                       */
+tri_status tri_rope(const tri_rope_config* cfg, const void* x, int64_t x_stride, void* y,
+                    int64_t y_stride, const int32_t* pos, int32_t n_tokens, int32_t n_heads,
+                    int32_t dtype, void* stream);
+
+/* 8-bit KV cache (device).  Rows, slots and pages as in tri_kv_cache; the panel P
+ * of a row is its slot (contiguous) or its page, of R = max_seq or block_size
+ * rows.  A value is code * scale with one scale per head and scale_rows
+ * consecutive rows of a panel (a scale block):
+ *  TRI_KV8_INT8  code an 8-bit integer in [-127, 127]
+ *  TRI_KV8_E4M3  code an 8-bit float of 4 exponent and 3 mantissa bits, at most 448
+ * A scale is a power of two, 2^-100 or more, so that codes move to a larger one by a
+ * shift.  A scale of NaN marks a block into which a value that is not finite was
+ * appended: every value of it is NaN.
+ * The library reads n_q_heads, n_kv_heads, head_dim (64 or 128) and dtype
+ * (TRI_BF16) of the tri_layer_config.                                           */
+typedef enum { TRI_KV8_INT8 = 0, TRI_KV8_E4M3 = 1 } tri_kv8_format;
+typedef struct {
+  void* k;                      /* codes [P, Hkv, R, D], one byte each, 16-byte
+                                   aligned                                        */
+  void* v;
+  float* k_scale;               /* [P, Hkv, ceil(R / scale_rows)]                 */
+  float* v_scale;
+  float* mass;                  /* [P, Hkv, R] accumulated attention weight of each
+                                   row, or NULL                                   */
+  int32_t* stamp;               /* [P, Hkv, R] position of the token in each row, or
+                                   NULL                                           */
+  int32_t n_slots;
+  int32_t max_seq;
+  const int32_t* block_table;   /* as in tri_kv_cache                             */
+  int32_t block_size;
+  int32_t n_blocks;
+  int32_t format;               /* tri_kv8_format                                 */
+  int32_t scale_rows;           /* 32, 64 or 128; paged: divides block_size       */
+} tri_kv8_cache;
+
+/* Append to an 8-bit cache: rows ctx_len[s] + i of slot[s] take the batch's new keys
+ * and values (rotated already).  Per head and scale block touched the scale becomes
+ * the least power of two s >= 2^-100 with max |x| <= 127 s (448 s) over the new rows,
+ * or the block's own scale where rows before ctx_len are held in it and that is
+ * larger; where it grew, the held codes are rounded once more (to nearest even, as
+ * the new ones).  The roundings of a value that was appended early add up to less
+ * than one step of the final scale.  Writes mass 0 and stamp pos[t] where the cache
+ * has them (pos[t] is needed then only; with more planes, the first).
+ *  k_new, v_new  device bf16 [T][Hkv][D], tokens `stride` elements apart (a multiple
+ *                of 8, >= Hkv D), 16-byte aligned
+ * A sequence with a slot out of range or rows past max_seq is skipped.           */
+tri_status tri_kv8_append(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                          const tri_batch* batch, const void* k_new, const void* v_new,
+                          int64_t stride, void* stream);
+
+/* Causal grouped-query attention over an 8-bit cache: token i of sequence s attends
+ * to rows 0 .. ctx_len[s] + i of its slot, which hold the batch's own rows already
+ * (tri_kv8_append first).  Any mix of chunks and single tokens.
+ *  q    device bf16 [T][Hq][D], tokens q_stride elements apart (a multiple of 8,
+ *       >= Hq D), 16-byte aligned;  Hq / Hkv <= 32
+ *  out  device bf16 [T][Hq][D]; must not overlap q
+ * Where the cache has `mass`, mass[row] += the row's attention weights summed over
+ * the KV head's query heads and the new tokens of the sequence (in one fixed order:
+ * the same inputs give the same sums).  Codes are exact in the products; scores,
+ * running maximum, sums and outputs are float32, attention weights rounded to 11 bits
+ * for the product with the values.  Tokens of a skipped sequence (as in the append)
+ * are left as they were.
+ * workspace: device, 256-byte aligned, of tri_kv8_attention_workspace_size bytes
+ * (the cache's and the batch's host fields are read; it never shrinks as max_ctx_len or
+ * n_tokens grows).                                                               */
+tri_status tri_kv8_attention_workspace_size(const tri_layer_config* cfg,
+                                            const tri_kv8_cache* cache, const tri_batch* batch,
+                                            size_t* bytes);
+tri_status tri_kv8_attention(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                             const tri_batch* batch, const void* q, int64_t q_stride, void* out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction, first half: which rows stay.  Of the n = ctx_len[s] + q_len rows of a
+ * sequence's slot, every KV head keeps `budget` (all where n <= budget): rows with
+ * stamp < n_first or stamp > newest - n_recent (newest: the largest stamp of the
+ * head's rows; row numbers stand in for stamps where the cache has none) before all
+ * others, those by descending mass, NaN last, ties to the lower row.  cache->mass is
+ * required.  A kept row below budget stays where it is; kept rows at or past budget
+ * take, in order, the places of evicted ones below it:
+ *  plan     device int32 [n_seqs][Hkv][budget]: row r is to hold what is in row
+ *           plan[r] (r itself where nothing changes, -1 past the rows held)
+ *  new_len  device int32 [n_seqs]: min(n, budget); or NULL
+ * budget: a multiple of scale_rows, <= max_seq; n_first, n_recent >= 0 with n_first +
+ * n_recent <= budget.  The rows kept are no longer in order of position: the stamps
+ * tell it, and keys are cached rotated, so attention does not mind.  A skipped
+ * sequence gets -1 throughout and new_len 0.                                      */
+tri_status tri_kv8_select(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                          const tri_batch* batch, int32_t budget, int32_t n_first,
+                          int32_t n_recent, int32_t* plan, int32_t* new_len, void* stream);
+
+/* Eviction, second half: row r of every KV head takes what is in row plan[r] (codes,
+ * mass, stamp), r < budget.  A scale block into which rows move takes the largest of
+ * its rows' scales; codes are shifted to it.  Rows at or past budget are left as they
+ * were, and a later append starts at new_len.  `batch` gives n_seqs and slots (as in
+ * the select).  An entry below 0 or at or past max_seq is left out; an entry r' != r
+ * must be >= budget.  A page shared between sequences must not be moved into.     */
+tri_status tri_kv8_move(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                        const tri_batch* batch, const int32_t* plan, int32_t budget,
+                        void* stream);
+
 /* Plain projection C = A B^T on the layer's GEMM kernels: the matrix
  * multiply of the Thinker's projections (Section II-A) and the synthetic
  * kernel of the paper's roofline benchmark over arithmetic intensity

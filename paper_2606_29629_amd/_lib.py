@@ -18,6 +18,9 @@ TRI_ERR_RANGE, TRI_ERR_ALIGN, TRI_ERR_WORKSPACE, TRI_ERR_HIP, TRI_ERR_ALIAS = -4
 TRI_ERR_SCRATCH = -9
 NOALLOC_SCRATCH_BYTES = 64 << 20
 TRI_BF16, TRI_F32 = 0, 1
+TRI_KV8_INT8, TRI_KV8_E4M3 = 0, 1
+TRI_ROPE_HALF, TRI_ROPE_INTERLEAVED = 0, 1
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}  # tri_rope_scaling
 TRI_F_QKV_BIAS, TRI_F_MOE, TRI_F_MOE_RENORM, TRI_F_QK_NORM, TRI_F_MROPE = 1, 2, 4, 8, 16
 
 
@@ -41,6 +44,19 @@ class KVCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_slots", ctypes.c_int32),
                 ("max_seq", ctypes.c_int32), ("block_table", ctypes.c_void_p),
                 ("block_size", ctypes.c_int32), ("n_blocks", ctypes.c_int32)]
+
+
+class KV8CacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "mass", "stamp")] + \
+               [("n_slots", ctypes.c_int32), ("max_seq", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("block_size", "n_blocks", "format", "scale_rows")]
+
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rotary_dim", "layout", "scaling",
+                                              "original_len")] + \
+               [(n, ctypes.c_float) for n in ("base", "factor", "low", "high", "magnitude")]
 
 
 class BatchStruct(ctypes.Structure):
@@ -98,6 +114,17 @@ _FUNCS = {
     "tri_linear_workspace_size": (ctypes.c_int, [ctypes.c_int32] * 3 + [ctypes.c_void_p]),
     "tri_linear": (ctypes.c_int, [ctypes.c_void_p] * 3 + [ctypes.c_int32] * 3
                    + [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "tri_rope": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                ctypes.c_int64, ctypes.c_void_p] + [ctypes.c_int32] * 3
+                 + [ctypes.c_void_p]),
+    "tri_kv8_append": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int64, ctypes.c_void_p]),
+    "tri_kv8_attention_workspace_size": (ctypes.c_int, [ctypes.c_void_p] * 4),
+    "tri_kv8_attention": (ctypes.c_int, [ctypes.c_void_p] * 4
+                          + [ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                             ctypes.c_void_p]),
+    "tri_kv8_select": (ctypes.c_int, [ctypes.c_void_p] * 3 + [ctypes.c_int32] * 3
+                       + [ctypes.c_void_p] * 3),
+    "tri_kv8_move": (ctypes.c_int, [ctypes.c_void_p] * 4 + [ctypes.c_int32, ctypes.c_void_p]),
 }
 
 
@@ -324,6 +351,211 @@ def linear(a, b, out=None, workspace=None, stream=None):
     _check(lib().tri_linear(_ptr(a), _ptr(b), _ptr(out), M, N, K, _ptr(workspace), wb,
                             _stream(stream)), "tri_linear")
     return out
+
+
+def make_rope(head_dim: int, rotary_dim: Optional[int] = None, base: float = 1e6,
+              interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
+              low: float = 1.0, high: float = 32.0, original_len: int = 0,
+              magnitude: float = 1.0) -> RopeConfig:
+    """RopeConfig of tri_rope; scaling: a key of ROPE_SCALING."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling {scaling!r}: one of {sorted(ROPE_SCALING)}")
+    return RopeConfig(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim),
+                      TRI_ROPE_INTERLEAVED if interleaved else TRI_ROPE_HALF,
+                      ROPE_SCALING[scaling], int(original_len), float(base), float(factor),
+                      float(low), float(high), float(magnitude))
+
+
+def _rows(x, what: str, last: int):
+    """Token stride of x [tokens, heads, last] whose heads are contiguous."""
+    if x.dim() != 3 or x.shape[2] != last or x.stride(2) != 1 or \
+            (x.shape[1] > 1 and x.stride(1) != last):
+        raise ValueError(f"{what}: [tokens, heads, {last}] with contiguous heads expected")
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * last)
+
+
+def _same_device(what: str, first, *others) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{what}: tensors on {first.device} and {t.device}")
+
+
+def _on_gpu(what: str, first, *others) -> None:
+    """The kernels follow plain addresses: every tensor of a call on the current GPU."""
+    import torch
+    _same_device(what, first, *others)
+    if not first.is_cuda or first.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: tensors on {first.device}, not on the current GPU")
+
+
+def rope(cfg: RopeConfig, x, pos, out=None, stream=None):
+    """x [tokens, heads, head_dim] (bf16 or float32, tokens any stride apart) with its
+    heads rotated to int32 positions pos [tokens] (tri_rope); out=x: in place."""
+    import torch
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if x.dtype not in (torch.bfloat16, torch.float32) or out.dtype != x.dtype:
+        raise ValueError(f"rope: bf16 or float32 in and out, got {x.dtype} and {out.dtype}")
+    if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() != x.shape[0]:
+        raise ValueError("rope: pos is a contiguous int32 [tokens]")
+    if out.shape != x.shape:
+        raise ValueError(f"rope: out {tuple(out.shape)}, x {tuple(x.shape)}")
+    _on_gpu("rope", x, pos, out)
+    xs, ys = _rows(x, "rope: x", cfg.head_dim), _rows(out, "rope: out", cfg.head_dim)
+    _check(lib().tri_rope(ctypes.byref(cfg), _ptr(x), xs, _ptr(out), ys, _ptr(pos), x.shape[0],
+                          x.shape[1], TRI_F32 if x.dtype == torch.float32 else TRI_BF16,
+                          _stream(stream)), "tri_rope")
+    return out
+
+
+class KV8Cache:
+    """An 8-bit KV cache (tri_kv8_cache): codes k, v [panels, Hkv, rows, D] (int8, or
+    float8_e4m3fn), a float32 scale per head and scale_rows rows, optionally the rows'
+    accumulated attention weight and their tokens' positions.  Contiguous (a panel is a slot),
+    or paged with block_table [n_slots, max_seq / rows] and max_seq."""
+
+    def __init__(self, k, v, k_scale, v_scale, scale_rows: int, mass=None, stamp=None,
+                 block_table=None, max_seq: Optional[int] = None):
+        import torch
+        formats = {torch.int8: TRI_KV8_INT8, torch.float8_e4m3fn: TRI_KV8_E4M3}
+        if k.dtype not in formats or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("KV8Cache: k and v are int8 or float8_e4m3fn [panels, Hkv, rows, D]")
+        panels, heads, rows = k.shape[:3]
+        per = -(-rows // int(scale_rows))
+        for name, t, shape, dt in (("k_scale", k_scale, (panels, heads, per), torch.float32),
+                                   ("v_scale", v_scale, (panels, heads, per), torch.float32),
+                                   ("mass", mass, (panels, heads, rows), torch.float32),
+                                   ("stamp", stamp, (panels, heads, rows), torch.int32)):
+            if t is None and name in ("mass", "stamp"):
+                continue
+            if t.dtype != dt or tuple(t.shape) != shape:
+                raise ValueError(f"KV8Cache: {name} is {dt} {shape}")
+        if block_table is None:
+            if max_seq is not None and max_seq > rows:
+                raise ValueError(f"KV8Cache: max_seq {max_seq} of {rows} rows")
+        elif max_seq is None or block_table.dtype != torch.int32 or \
+                block_table.dim() != 2 or block_table.shape[1] * rows != max_seq:
+            raise ValueError("KV8Cache: block_table is int32 [n_slots, max_seq / rows]")
+        tensors = (k, v, k_scale, v_scale, mass, stamp, block_table)
+        if not all(t is None or t.is_contiguous() for t in tensors):
+            raise ValueError("KV8Cache: contiguous tensors expected")
+        _same_device("KV8Cache", *tensors)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.mass, self.stamp, self.block_table = mass, stamp, block_table
+        self.scale_rows, self.head_dim, self.n_kv_heads = int(scale_rows), int(k.shape[3]), int(heads)
+        paged = block_table is not None
+        self.n_slots = int(block_table.shape[0]) if paged else int(panels)
+        self.max_seq = int(max_seq) if paged else int(rows)
+        self._struct = KV8CacheStruct(*[_ptr(t) for t in tensors[:6]], self.n_slots, self.max_seq,
+                                      _ptr(block_table), int(rows) if paged else 0,
+                                      int(panels) if paged else 0, formats[k.dtype], self.scale_rows)
+
+    @classmethod
+    def empty(cls, cfg: LayerConfig, n_slots: int, max_seq: int, format: str = "int8",
+              scale_rows: int = 32, mass: bool = False, stamp: bool = False, block_table=None,
+              block_size: int = 0, n_blocks: int = 0, device="cuda"):
+        """A cache without rows: contiguous, or paged with a block_table."""
+        import torch
+        dt = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[format]
+        paged = block_table is not None
+        panels, rows = (n_blocks, block_size) if paged else (n_slots, max_seq)
+        shape = panels, cfg.n_kv_heads, rows
+        codes = [torch.zeros(*shape, cfg.head_dim, dtype=torch.uint8, device=device).view(dt)
+                 for _ in range(2)]
+        scales = [torch.ones(panels, cfg.n_kv_heads, -(-rows // scale_rows), device=device)
+                  for _ in range(2)]
+        return cls(*codes, *scales, scale_rows,
+                   mass=torch.zeros(shape, device=device) if mass else None,
+                   stamp=torch.zeros(shape, dtype=torch.int32, device=device) if stamp else None,
+                   block_table=block_table, max_seq=max_seq if paged else None)
+
+    def struct(self) -> KV8CacheStruct:
+        return self._struct
+
+
+def _kv8(what, cfg, cache, batch, *tensors):
+    if (cfg.n_kv_heads, cfg.head_dim) != (cache.n_kv_heads, cache.head_dim):
+        raise ValueError(f"{what}: the cache has {cache.n_kv_heads} heads of {cache.head_dim}, "
+                         f"the layer {cfg.n_kv_heads} of {cfg.head_dim}")
+    _on_gpu(what, cache.k, batch.slot, *tensors)
+    return ctypes.byref(cfg), ctypes.byref(cache.struct()), ctypes.byref(batch.struct())
+
+
+def kv8_append(cfg, cache: KV8Cache, batch, k_new, v_new, stream=None) -> None:
+    """The batch's new keys (rotated) and values [tokens, Hkv, D] (bf16, tokens any one
+    stride apart) into the 8-bit cache (tri_kv8_append)."""
+    import torch
+    stride = _rows(k_new, "kv8_append: k_new", cfg.head_dim)
+    shape = (batch.n_tokens, cfg.n_kv_heads, cfg.head_dim)
+    if tuple(k_new.shape) != shape or tuple(v_new.shape) != shape or \
+            _rows(v_new, "kv8_append: v_new", cfg.head_dim) != stride:
+        raise ValueError(f"kv8_append: k_new and v_new are {shape} with one token stride")
+    if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
+        raise ValueError("kv8_append: k_new and v_new are bf16")
+    _check(lib().tri_kv8_append(*_kv8("kv8_append", cfg, cache, batch, k_new, v_new), _ptr(k_new),
+                                _ptr(v_new), stride, _stream(stream)), "tri_kv8_append")
+
+
+def kv8_attention_workspace_size(cfg, cache: KV8Cache, batch) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().tri_kv8_attention_workspace_size(
+        ctypes.byref(cfg), ctypes.byref(cache.struct()), ctypes.byref(batch.struct()),
+        ctypes.byref(n)), "tri_kv8_attention_workspace_size")
+    return n.value
+
+
+def kv8_attention(cfg, cache: KV8Cache, batch, q, out=None, workspace=None, stream=None):
+    """Causal attention of q [tokens, Hq, D] (bf16, tokens any stride apart) over the 8-bit
+    cache, adding up cache.mass where it has one (tri_kv8_attention); returns (out, workspace)."""
+    import torch
+    shape = (batch.n_tokens, cfg.n_q_heads, cfg.head_dim)
+    if tuple(q.shape) != shape or q.dtype != torch.bfloat16:
+        raise ValueError(f"kv8_attention: q is bf16 {shape}")
+    stride = _rows(q, "kv8_attention: q", cfg.head_dim)
+    if out is None:
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+    if tuple(out.shape) != shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError(f"kv8_attention: out is contiguous bf16 {shape}")
+    if workspace is None:
+        workspace = torch.empty(kv8_attention_workspace_size(cfg, cache, batch),
+                                dtype=torch.uint8, device=q.device)
+    args = _kv8("kv8_attention", cfg, cache, batch, q, out, workspace)
+    _check(lib().tri_kv8_attention(*args, _ptr(q), stride, _ptr(out), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream)),
+           "tri_kv8_attention")
+    return out, workspace
+
+
+def kv8_select(cfg, cache: KV8Cache, batch, budget: int, n_first: int = 0, n_recent: int = 0,
+               plan=None, new_len=None, stream=None):
+    """Which rows of the batch's sequences (ctx_len + q_len each) stay within budget
+    (tri_kv8_select); returns (plan [n_seqs, Hkv, budget], new_len [n_seqs]), int32."""
+    import torch
+    shape = (batch.n_seqs, cfg.n_kv_heads, int(budget))
+    if plan is None:
+        plan = torch.empty(shape, dtype=torch.int32, device=cache.k.device)
+    if new_len is None:
+        new_len = torch.empty(batch.n_seqs, dtype=torch.int32, device=cache.k.device)
+    _plan("kv8_select", plan, shape)
+    if new_len.dtype != torch.int32 or new_len.numel() != batch.n_seqs or not new_len.is_contiguous():
+        raise ValueError(f"kv8_select: new_len is a contiguous int32 [{batch.n_seqs}]")
+    _check(lib().tri_kv8_select(*_kv8("kv8_select", cfg, cache, batch, plan, new_len), int(budget),
+                                int(n_first), int(n_recent), _ptr(plan), _ptr(new_len),
+                                _stream(stream)), "tri_kv8_select")
+    return plan, new_len
+
+
+def _plan(what, plan, shape):
+    import torch
+    if plan.dtype != torch.int32 or tuple(plan.shape) != tuple(shape) or not plan.is_contiguous():
+        raise ValueError(f"{what}: plan is a contiguous int32 {tuple(shape)}")
+
+
+def kv8_move(cfg, cache: KV8Cache, batch, plan, stream=None) -> None:
+    """Rows of the batch's sequences to the places of a kv8_select plan (tri_kv8_move)."""
+    _plan("kv8_move", plan, (batch.n_seqs, cfg.n_kv_heads, plan.shape[-1]))
+    _check(lib().tri_kv8_move(*_kv8("kv8_move", cfg, cache, batch, plan), _ptr(plan),
+                              int(plan.shape[-1]), _stream(stream)), "tri_kv8_move")
 
 
 def moe_route(cfg, h2_f32, w_router, idx, w, stream=None) -> None:

@@ -195,6 +195,43 @@ hipError_t launch_attn_decode_combine(const float* part, void* out, const BatchD
                                       const KvDev& kv, int n_q_heads, int n_kv_heads,
                                       int head_dim, hipStream_t s);
 
+// Rotary positions (tri_rope): per pair its turns per position, f / 2 pi.
+constexpr int kRopeMaxPairs = 128;
+struct RopeDev {
+  double turns[kRopeMaxPairs];
+  int rot, head_dim, n_heads;
+  float magnitude;
+};
+hipError_t launch_rope(const RopeDev& r, bool interleaved, const void* x, int64_t xs, void* y,
+                       int64_t ys, const int32_t* pos, int n_tokens, bool f32, hipStream_t s);
+
+// 8-bit KV cache: rows addressed as in KvDev, one byte per value, one scale per head
+// and 2^scale_shift rows of a panel.
+struct Kv8Dev {
+  KvDev kv;
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  float* mass;     // nullable
+  int32_t* stamp;  // nullable
+  int scale_shift;
+  __host__ __device__ int scales_per_panel() const {
+    return (kv.panel_rows() + (1 << scale_shift) - 1) >> scale_shift;
+  }
+};
+hipError_t launch_kv8_append(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_kv_heads,
+                             int head_dim, const void* k_new, const void* v_new, int64_t stride,
+                             hipStream_t s);
+size_t attn_kv8_workspace_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads, int n_kv_heads,
+                                int head_dim);
+hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q_heads,
+                           int n_kv_heads, int head_dim, const void* q, int64_t q_stride, void* out,
+                           void* ws, hipStream_t s);
+hipError_t launch_kv8_select(const BatchDev& b, const Kv8Dev& c, int n_kv_heads, int budget,
+                             int n_first, int n_recent, int32_t* plan, int32_t* new_len,
+                             hipStream_t s);
+hipError_t launch_kv8_move(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_kv_heads,
+                           int head_dim, const int32_t* plan, int budget, hipStream_t s);
+
 // Mixture of experts.  Grouped GEMM over experts: rows [seg[e], seg[e+1]) of
 // the routed order belong to expert e; the gate/up pass gathers A rows
 // perm[p] / top_k (perm = routed pair ids), the down pass reads A rows in
