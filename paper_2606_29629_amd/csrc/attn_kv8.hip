@@ -7,7 +7,7 @@
 // scores, then D threads over the values, with the running maximum and sum of the
 // softmax in float32.  The log-sum-exp of every (token, head) goes to the workspace,
 // from which a second kernel forms the weights again, row by row, and sums them.
-#include "kv8.hpp"
+#include "attn_kv8.hpp"
 
 namespace tri {
 
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void attn_kv8_kernel(BatchDev b, Kv8Dev c, int
   int s = 0;
   while (s < b.n_seqs - 1 && b.cu_q[s + 1] <= t) ++s;
   int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || t < q0 || t >= q0 + n) return;
+  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || t < q0 || t >= q0 + n || n == 1) return;
   const int h = hq / (Hq / Hkv), rows = ctx + (t - q0) + 1;
   if (tid < D) qv[tid] = bf2f(q[(int64_t)t * qs + (int64_t)hq * D + tid]);
   float m = -INFINITY, l = 0.f, acc = 0.f;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void mass_kv8_kernel(BatchDev b, Kv8Dev c, int
   __shared__ float qv[D];
   const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
   int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n == 0) return;
+  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n <= 1) return;
   const int r = blockIdx.x * 256 + tid, G = Hq / Hkv;
   int prow, panel = -1;
   if (r < ctx + n) panel = kv_panel(c.kv, sl, r, prow);
@@ -118,7 +118,8 @@ __global__ __launch_bounds__(256) void mass_kv8_kernel(BatchDev b, Kv8Dev c, int
 
 size_t attn_kv8_workspace_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads, int n_kv_heads,
                                 int head_dim) {
-  return c.mass ? (size_t)b.n_tokens * n_q_heads * sizeof(float) : 0;
+  const size_t lse = c.mass ? (size_t)b.n_tokens * n_q_heads * sizeof(float) : 0;
+  return (lse + 255) / 256 * 256 + attn_kv8_decode_bytes(b, c, n_q_heads, n_kv_heads, head_dim);
 }
 
 hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q_heads,
@@ -127,6 +128,12 @@ hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q
   if (b.n_seqs == 0 || b.n_tokens == 0) return hipSuccess;
   const float scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)head_dim));
   float* lse = c.mass ? (float*)ws : nullptr;
+  const size_t lse_bytes = c.mass ? (size_t)b.n_tokens * n_q_heads * sizeof(float) : 0;
+  if (b.max_q_len == 1 || (int64_t)b.n_seqs * b.max_q_len != b.n_tokens) {
+    const hipError_t e = launch_attn_kv8_decode(b, c, fp8, n_q_heads, n_kv_heads, head_dim, q, q_stride, out,
+                                                (float*)((char*)ws + (lse_bytes + 255) / 256 * 256), s);
+    if (e != hipSuccess || b.max_q_len == 1) return e;
+  }
   auto go = [&](auto attend, auto weigh) {
     attend<<<dim3(b.n_tokens, n_q_heads), 256, 0, s>>>(b, c, n_q_heads, n_kv_heads, (const bf16*)q,
                                                        q_stride, (bf16*)out, lse, scale_log2e);
