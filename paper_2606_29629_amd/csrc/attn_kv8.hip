@@ -1,153 +1,522 @@
-// Causal grouped-query attention over the 8-bit cache.
+// Causal flash attention of chunks (sequences of two tokens or more) over the 8-bit
+// cache, and the sums of their attention weights.
 //
-// out = sum_j p_j v_j, p = softmax(q k_j / sqrt D) over rows j <= ctx + i; with mass,
-// mass[j] += p_j summed over the KV head's query heads and the new tokens.
+// The query rows of a KV head are its tokens times the group's G query heads, packed: row
+// x is head x % G of token x / G.  So K and V are read and converted once for the whole
+// group, a chunk of a few tokens fills a tile, and the causal edge crosses few rows of it.
+// One workgroup = 128 rows, 4 waves of 32; 64 cache rows per tile.  Two products of 64 x
+// 32 x D per wave and tile bound it (32 matrix instructions, 1024 cycles at D = 128);
+// beside them 32 exponentials a lane and the tile's fragments out of LDS.
 //
-// One workgroup per (query head, token): 256 rows a step, a row per thread for the
-// scores, then D threads over the values, with the running maximum and sum of the
-// softmax in float32.  The log-sum-exp of every (token, head) goes to the workspace,
-// from which a second kernel forms the weights again, row by row, and sums them.
+// A tile's codes go to registers two tiles ahead, are converted to float16 once per
+// workgroup (exact: attn_kv8.hpp) and written to LDS one tile ahead, chunks swizzled by
+// kv_chunk, double buffered, one barrier per tile.  S^T = K Q^T and O^T += V^T P'^T on
+// v_mfma_f32_32x32x16_f16: a lane owns one query row and 32 of the tile's 64 keys, its
+// weights are the second product's operand where they are, and V is transposed by
+// ds_read_b64_tr_b16.  Value scales ride in the weights' exponent as in the single-token
+// kernel, one float16 rounding (2^-11) per weight.
+#include <type_traits>
+
 #include "attn_kv8.hpp"
 
 namespace tri {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kRows8 = 128;    // packed query rows per workgroup
+constexpr int kKeys8 = 64;     // cache rows per tile
+constexpr int kMaxSplitF8 = 8;  // key-range splits of a row tile, at most
 
-// q . (codes of row `at`), D values, q in LDS
-template <int D, bool FP8>
-__device__ __forceinline__ float dot_row(const uint8_t* codes, const float* q) {
-  float s = 0.f;
-#pragma unroll
-  for (int d = 0; d < D; d += 16) {
-    const u32x4 c = ldg16(codes + d);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 v = kv8_decode4<FP8>(c[j]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s = fmaf(v[e], q[d + 4 * j + e], s);
-    }
+// Thread i of 256 (and 256 more for D = 128) moves 16 codes of a tile: row and chunk, rows
+// ordered so that 16 neighbouring threads' float16 chunks fall on different banks (the
+// swizzle of rows 4 apart differs in parity).
+template <int D>
+__device__ __forceinline__ void stage_place(int i, int& row, int& chunk) {
+  if constexpr (D == 128) {
+    const int r = i >> 3;
+    chunk = i & 7;
+    row = (r & ~7) | ((r & 1) << 2) | ((r & 7) >> 1);
+  } else {
+    const int r = i >> 2;
+    chunk = i & 3;
+    row = (r & ~7) | ((r & 2) << 1) | ((r & 4) >> 1) | (r & 1);
   }
-  return s;
 }
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(256) void attn_kv8_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
-                                                       const bf16* __restrict__ q, int64_t qs,
-                                                       bf16* __restrict__ out,
-                                                       float* __restrict__ lse, float scale_log2e) {
-  __shared__ float qv[D], p[256], vscale[256], red[4];
-  __shared__ int64_t vrow[256];
-  const int t = blockIdx.x, hq = blockIdx.y, tid = threadIdx.x;
-  int s = 0;
-  while (s < b.n_seqs - 1 && b.cu_q[s + 1] <= t) ++s;
+template <int D, bool FP8, bool PAGED, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
+                                                          const bf16* __restrict__ Q, int64_t qs,
+                                                          bf16* __restrict__ O,
+                                                          float* __restrict__ lse,
+                                                          float* __restrict__ part, int nsplit,
+                                                          float scale_log2e) {
+  constexpr int DS = D / 16, DB = D / 32;
+  constexpr int NL = D / 64;  // 16-code loads of a thread, operand and tile
+  __shared__ __align__(16) f16 sk[2][kKeys8 * D], sv[2][kKeys8 * D];
+
+  // the rows with the most keys first, over all heads and sequences
+  const int per = Hkv * b.n_seqs * nsplit;
+  const int tile = (int)(gridDim.x / per) - 1 - (int)(blockIdx.x / per);
+  int rest = blockIdx.x % per;
+  const int h = rest % Hkv;
+  rest /= Hkv;
+  const int s = rest / nsplit, sp = rest - s * nsplit;
   int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || t < q0 || t >= q0 + n || n == 1) return;
-  const int h = hq / (Hq / Hkv), rows = ctx + (t - q0) + 1;
-  if (tid < D) qv[tid] = bf2f(q[(int64_t)t * qs + (int64_t)hq * D + tid]);
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  for (int r0 = 0; r0 < rows; r0 += 256) {
-    __syncthreads();
-    const int r = r0 + tid;
-    float sc = -INFINITY;
-    vrow[tid] = -1;
-    if (r < rows) {
-      int prow;
-      const int panel = kv_panel(c.kv, sl, r, prow);
-      sc = 0.f;
-      if (panel >= 0) {
-        const int64_t at = kv8_row_at(c, Hkv, panel, h, prow), sa = kv8_scale_at(c, Hkv, panel, h, prow);
-        sc = dot_row<D, FP8>(c.k + at * D, qv) * c.k_scale[sa] * scale_log2e;
-        vrow[tid] = at;
-        vscale[tid] = c.v_scale[sa];
+  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2) return;
+  const int G = Hq / Hkv, rows = n * G, row0 = tile * kRows8;
+  if (row0 >= rows) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lg = lane >> 5;
+  const int kv_len = ctx + (min(rows, row0 + kRows8) - 1) / G + 1;
+  const int nkt = cdiv(kv_len, kKeys8);
+  const int tps = SPLIT ? cdiv(nkt, nsplit) : nkt;
+  const int kt_lo = sp * tps, kt_hi = min(nkt, kt_lo + tps);
+  if (kt_lo >= kt_hi) return;  // (the merge skips an empty split)
+
+  const int prows = c.kv.panel_rows(), spp = c.scales_per_panel();
+  struct Place {
+    int panel, prow;
+  };
+  auto place = [&](int kt) {
+    Place p{sl, kt * kKeys8};
+    if (PAGED && kt < nkt) p.panel = kv_panel(c.kv, sl, kt * kKeys8, p.prow);
+    return p;
+  };
+  int st_row[NL], st_chunk[NL];
+#pragma unroll
+  for (int j = 0; j < NL; ++j) stage_place<D>(tid + 256 * j, st_row[j], st_chunk[j]);
+  u32x4 kraw[NL], vraw[NL];
+  float ks_next[2], vs_next[2];  // the scales of the tile in kraw, vraw
+  auto gload = [&](int kt) {
+    Place p = place(kt);
+    int live = min(kKeys8, kv_len - kt * kKeys8);
+    if (p.panel < 0 || live <= 0) live = p.panel = p.prow = 0;
+    const int64_t head = (int64_t)p.panel * Hkv + h;
+    const int64_t at = (head * prows + p.prow) * D;
+    const auto rk = __builtin_amdgcn_make_buffer_rsrc((void*)(c.k + at), (short)0, live * D, 0x00020000);
+    const auto rv = __builtin_amdgcn_make_buffer_rsrc((void*)(c.v + at), (short)0, live * D, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int off = st_row[j] * D + st_chunk[j] * 16;
+      kraw[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
+      vraw[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bool seen = 32 * u < live;  // (scales of rows past the end are not looked at)
+      const int64_t sa = head * spp + ((p.prow + (seen ? 32 * u : 0)) >> c.scale_shift);
+      ks_next[u] = seen ? c.k_scale[sa] : 1.f;
+      vs_next[u] = seen ? c.v_scale[sa] : 1.f;
+    }
+  };
+  float ks[2], vs[2];
+  auto convert = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int r = st_row[j], c0 = 2 * st_chunk[j];
+      f16* kd = sk[buf] + r * D;
+      f16* vd = sv[buf] + r * D;
+      const int p0 = kv_chunk<D>(c0, r) * 8, p1 = kv_chunk<D>(c0 + 1, r) * 8;
+      *(f16x8*)(kd + p0) = codes_to_f16<FP8>(kraw[j][0], kraw[j][1]);
+      *(f16x8*)(kd + p1) = codes_to_f16<FP8>(kraw[j][2], kraw[j][3]);
+      *(f16x8*)(vd + p0) = codes_to_f16<FP8>(vraw[j][0], vraw[j][1]);
+      *(f16x8*)(vd + p1) = codes_to_f16<FP8>(vraw[j][2], vraw[j][3]);
+    }
+  };
+
+  // This lane's query row (rows past the end repeat the last one and are not written).
+  const int row = row0 + wave * 32 + lr, rc = min(row, rows - 1);
+  const int tok = rc / G, hq = h * G + rc - tok * G;
+  const int qpos = ctx + tok;
+  const int wave_lo = ctx + min(row0 + wave * 32, rows - 1) / G;  // first and last token of the wave
+  const int wave_hi = ctx + min(row0 + wave * 32 + 31, rows - 1) / G;
+  f16x8 qf[DS];
+  float score_scale;
+  gload(kt_lo);
+  {
+    Pack8 x[DS];
+    const bf16* qp = Q + (int64_t)(q0 + tok) * qs + (int64_t)hq * D + 8 * lg;
+#pragma unroll
+    for (int t = 0; t < DS; ++t) x[t].u = ldg16(qp + 16 * t);
+    score_scale = q_to_f16<32>(x, qf) * scale_log2e;
+  }
+  const int tr_key = 4 * lg + ((lane & 15) >> 2);
+  const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) oacc[d] = f32x16{0.f};
+  float m_run = -INFINITY, l_run = 0.f;  // log2 units
+
+  convert(0);
+  ks[0] = ks_next[0], ks[1] = ks_next[1], vs[0] = vs_next[0], vs[1] = vs_next[1];
+  if (kt_lo + 1 < kt_hi) gload(kt_lo + 1);
+
+  auto step = [&](int kt, auto buf) {
+    __syncthreads();  // tile kt is in LDS; every wave is done with tile kt - 1
+    float ks_after[2] = {ks_next[0], ks_next[1]}, vs_after[2] = {vs_next[0], vs_next[1]};
+    if (kt + 1 < kt_hi) convert(1 - decltype(buf)::value);
+    if (kt + 2 < kt_hi) gload(kt + 2);
+    const f16* kb_lds = sk[decltype(buf)::value];
+    const f16* vb = sv[decltype(buf)::value];
+    const int key0 = kt * kKeys8;
+    if (key0 <= wave_hi) {  // (else no key of this tile is visible to this wave)
+      constexpr int KLA = 3;
+      f32x16 sacc[2] = {f32x16{0.f}, f32x16{0.f}};
+      f16x8 kf[KLA + 1][2];
+      auto kread = [&](int t, f16x8 (&dst)[2]) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const int key = kb * 32 + lr;
+          dst[kb] = *(const f16x8*)&kb_lds[key * D + kv_chunk<D>(2 * t + lg, key) * 8];
+        }
+      };
+#pragma unroll
+      for (int t = 0; t < KLA && t < DS; ++t) kread(t, kf[t]);
+#pragma unroll
+      for (int t = 0; t < DS; ++t) {
+        if (t + KLA < DS) kread(t + KLA, kf[(t + KLA) % (KLA + 1)]);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+          sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[t % (KLA + 1)][kb], qf[t], sacc[kb], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      union VFrag {
+        s16x4 s[2];
+        f16x8 h;
+      };
+      VFrag vf[2][DB];
+      auto vread = [&](int g16, VFrag (&dst)[DB]) {
+        const int k1 = 16 * g16 + tr_key, k2 = k1 + 8;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int col = 32 * d + tr_col;
+          dst[d].s[0] = lds_read_tr16((const bf16*)(vb + k1 * D + kv_chunk<D>(col >> 3, k1) * 8 + (col & 7)));
+          dst[d].s[1] = lds_read_tr16((const bf16*)(vb + k2 * D + kv_chunk<D>(col >> 3, k2) * 8 + (col & 7)));
+        }
+      };
+      vread(0, vf[0]);
+      // scores in log2 units: kf s + ve
+      float kfac[2], ve[2], vinv[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const float f = ks[kb] * score_scale;
+        kfac[kb] = f < 1.17549435e-38f ? 1.17549435e-38f : f;  // (not 0: -inf * 0)
+        ve[kb] = scale_log2(vs[kb]);
+        vinv[kb] = scale_inverse(vs[kb]);
+      }
+      if (key0 + kKeys8 - 1 > wave_lo) {  // the causal edge crosses this tile
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = key0 + 32 * kb + (e & 3) + 8 * (e >> 2) + 4 * lg;
+            if (key > qpos) sacc[kb][e] = -INFINITY;
+          }
+          // a block past this row: none of its scales either (one may be NaN)
+          const bool none = key0 + 32 * kb > qpos;
+          kfac[kb] = none ? 1.f : kfac[kb];
+          ve[kb] = none ? 0.f : ve[kb];
+          vinv[kb] = none ? 1.f : vinv[kb];
+        }
+      }
+      const float thr = m_run + kSoftmaxSlack;
+      const float mh = fmaxf(fmaf(tree_max16(sacc[0]), kfac[0], ve[0]), fmaf(tree_max16(sacc[1]), kfac[1], ve[1]));
+      if (__builtin_amdgcn_ballot_w64(mh > thr)) {
+        const float mt = fmaxf(mh, __shfl_xor(mh, 32, 64));
+        const bool raise = mt > thr;
+        const float m_new = raise ? mt : m_run;
+        const float alpha = raise ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) oacc[d] *= alpha;
+      }
+      // (a row that precedes every key so far has no maximum; its weights are 0)
+      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+      f16x8 p[4];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const float off = ve[kb] - m_use;
+        float ls[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(sacc[kb][8 * u + e], kfac[kb], off));
+          ls[u] = tree_sum8(w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[2 * kb + u][e] = (f16)w[e];
+        }
+        l_run = fmaf(ls[0] + ls[1], vinv[kb], l_run);
+      }
+#pragma unroll
+      for (int g16 = 0; g16 < 4; ++g16) {
+        if (g16 + 1 < 4) vread(g16 + 1, vf[(g16 + 1) & 1]);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+          oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[g16 & 1][d].h, p[g16], oacc[d], 0, 0, 0);
       }
     }
-    float mt = wave_max(sc);
-    if ((tid & 63) == 0) red[tid >> 6] = mt;
-    __syncthreads();
-    const float mn = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), m);
-    const float a = exp2f(m - mn), w = exp2f(sc - mn);
-    p[tid] = w;
-    const float lt = wave_sum(w);
-    __syncthreads();
-    if ((tid & 63) == 0) red[tid >> 6] = lt;
-    __syncthreads();
-    l = l * a + (red[0] + red[1] + red[2] + red[3]);
-    m = mn;
-    if (tid < D) {
-      acc *= a;
-      for (int j = 0; j < min(256, rows - r0); ++j) {
-        if (vrow[j] < 0) continue;
-        const uint32_t word = c.v[vrow[j] * D + tid];
-        acc = fmaf(p[j] * vscale[j], kv8_decode4<FP8>(word)[0], acc);
+    ks[0] = ks_after[0], ks[1] = ks_after[1], vs[0] = vs_after[0], vs[1] = vs_after[1];
+  };
+  for (int kt = kt_lo; kt < kt_hi; kt += 2) {
+    step(kt, Int<0>{});
+    if (kt + 1 < kt_hi) step(kt + 1, Int<1>{});
+  }
+
+  const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+  if (row >= rows) return;
+  // packed rows of all sequences in order: q0 G + row
+  const int64_t at = (int64_t)h * b.n_tokens * G + (int64_t)q0 * G + row;
+  if constexpr (SPLIT) {
+    float* pp = part + ((int64_t)sp * b.n_tokens * Hq + at) * (D + 4);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *(f32x4*)(pp + 32 * d + 8 * r4 + 4 * lg) =
+            f32x4{oacc[d][4 * r4], oacc[d][4 * r4 + 1], oacc[d][4 * r4 + 2], oacc[d][4 * r4 + 3]};
+    if (lg == 0) *(f32x2*)(pp + D) = f32x2{m_run, l_tot};
+    return;
+  }
+  const float inv = 1.0f / l_tot;
+  bf16* op = O + ((int64_t)(q0 + tok) * Hq + hq) * D;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = f2bf(oacc[d][4 * r4 + e] * inv);
+      *(bf16x4*)(op + 32 * d + 8 * r4 + 4 * lg) = o;
+    }
+  if (lse && lg == 0) lse[at] = m_run + log2f(l_tot);
+}
+
+// Merge of the key-range splits, D / 4 threads per packed row, folded in split order.
+template <int D>
+__global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
+                                                            const float* __restrict__ part,
+                                                            bf16* __restrict__ O,
+                                                            float* __restrict__ lse, int nsplit) {
+  constexpr int TPR = D / 4;
+  const int s = blockIdx.z, h = blockIdx.y, G = Hq / Hkv;
+  int q0, n, ctx, sl;
+  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2) return;
+  const int row = blockIdx.x * (256 / TPR) + (int)threadIdx.x / TPR, rows = n * G;
+  if (row >= rows) return;
+  const int last = min(rows, (row / kRows8 + 1) * kRows8) - 1;  // of the flash kernel's tile
+  const int nkt = cdiv(ctx + last / G + 1, kKeys8), ns = cdiv(nkt, cdiv(nkt, nsplit));
+  const int64_t at = (int64_t)h * b.n_tokens * G + (int64_t)q0 * G + row;
+  const int64_t plane = (int64_t)b.n_tokens * Hq * (D + 4);
+  const float* pp = part + at * (D + 4);
+  const int d = 4 * ((int)threadIdx.x % TPR);
+  f32x2 ml[kMaxSplitF8];
+  f32x4 a[kMaxSplitF8];
+#pragma unroll
+  for (int j = 0; j < kMaxSplitF8; ++j) {  // (splits past the last are loaded again and dropped)
+    const float* pj = pp + min(j, ns - 1) * plane;
+    ml[j] = *(const f32x2*)(pj + D);
+    a[j] = *(const f32x4*)(pj + d);
+  }
+  float M = -INFINITY, L = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kMaxSplitF8; ++j) {
+    if (j >= ns || (ml[j][0] == -INFINITY && ml[j][1] == 0.f)) continue;  // no key of it visible
+    const float Mn = fmaxf(M, ml[j][0]);
+    const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[j][0] - Mn);
+    L = L * x + ml[j][1] * w;
+    o = o * x + a[j] * w;
+    M = Mn;
+  }
+  const int tok = row / G, hq = h * G + row - tok * G;
+  bf16x4 o4;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o4[e] = f2bf(o[e] / L);
+  *(bf16x4*)(O + ((int64_t)(q0 + tok) * Hq + hq) * D + d) = o4;
+  if (lse && d == 0) lse[at] = M + log2f(L);
+}
+
+// mass[key] += sum over the packed rows of 2^(score - lse): the scores once more, keys and
+// rows the other way round.  One workgroup = 128 cache rows of a KV head, a wave 32 of
+// them with their codes in registers as bf16 (exact too, and q needs no conversion); rows
+// come 64 at a time through LDS by direct loads.  Every sum has one owner and one order.
+constexpr int kMassKeys = 128, kMassQ = 64;
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(256, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
+                                                               const bf16* __restrict__ Q, int64_t qs,
+                                                               const float* __restrict__ lse,
+                                                               float scale_log2e) {
+  constexpr int DS = D / 16, DC = D / 8;
+  constexpr int RPB = 64 / DC;             // rows of a 1 KB load
+  constexpr int NL = kMassQ / RPB / 4;     // such loads of a wave and tile
+  __shared__ __align__(16) bf16 sq0[kMassQ * D], sq1[kMassQ * D];
+  const int s = blockIdx.z, h = blockIdx.y, key0 = blockIdx.x * kMassKeys;
+  int q0, n, ctx, sl;
+  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2 || key0 >= ctx + n) return;
+  const int G = Hq / Hkv, rows = n * G;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lg = lane >> 5;
+  // codes of this wave's 32 keys: lane key lr, values 16 t + 8 lg ...
+  const int wkey = key0 + 32 * wave;
+  int prow = 0;
+  const int panel = wkey < ctx + n ? kv_panel(c.kv, sl, wkey, prow) : -1;
+  const int live = panel < 0 ? 0 : min(32, ctx + n - wkey);
+  float kf = 0.f;
+  bf16x8 kreg[DS];
+  {
+    const int64_t head = (int64_t)max(panel, 0) * Hkv + h;
+    if (live > 0) kf = c.k_scale[head * c.scales_per_panel() + (prow >> c.scale_shift)] * scale_log2e;
+    const auto rk = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(c.k + (head * c.kv.panel_rows() + prow) * D), (short)0, live * D, 0x00020000);
+#pragma unroll
+    for (int t = 0; t < DS; ++t) {
+      const auto w = __builtin_amdgcn_raw_buffer_load_b64(rk, lr * D + 16 * t + 8 * lg, 0, 0);
+      const f32x4 lo = kv8_decode4<FP8>(w[0]), hi = kv8_decode4<FP8>(w[1]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        kreg[t][e] = f2bf(lo[e]);
+        kreg[t][4 + e] = f2bf(hi[e]);
       }
     }
   }
-  if (tid < D) out[((int64_t)t * Hq + hq) * D + tid] = f2bf(acc / l);
-  if (lse && tid == 0) lse[(int64_t)t * Hq + hq] = m + log2f(l);
-}
-
-template <int D, bool FP8>
-__global__ __launch_bounds__(256) void mass_kv8_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
-                                                       const bf16* __restrict__ q, int64_t qs,
-                                                       const float* __restrict__ lse,
-                                                       float scale_log2e) {
-  __shared__ float qv[D];
-  const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
-  int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n <= 1) return;
-  const int r = blockIdx.x * 256 + tid, G = Hq / Hkv;
-  int prow, panel = -1;
-  if (r < ctx + n) panel = kv_panel(c.kv, sl, r, prow);
-  int64_t at = 0;
-  float ks = 0.f, sum = 0.f;
-  if (panel >= 0) {
-    at = kv8_row_at(c, Hkv, panel, h, prow);
-    ks = c.k_scale[kv8_scale_at(c, Hkv, panel, h, prow)] * scale_log2e;
-  }
-  for (int i = 0; i < n; ++i)
-    for (int g = 0; g < G; ++g) {
-      const int hq = h * G + g;
-      __syncthreads();
-      if (tid < D) qv[tid] = bf2f(q[(int64_t)(q0 + i) * qs + (int64_t)hq * D + tid]);
-      __syncthreads();
-      if (panel >= 0 && r <= ctx + i)
-        sum += exp2f(dot_row<D, FP8>(c.k + at * D, qv) * ks - lse[(int64_t)(q0 + i) * Hq + hq]);
+  // row tiles from the first that sees key0
+  const int rt_lo = max(0, key0 - ctx) * G / kMassQ, rt_hi = cdiv(rows, kMassQ);
+  auto gload = [&](int rt, auto buf) {
+    bf16* dst = decltype(buf)::value ? sq1 : sq0;
+    const int tok0 = rt * kMassQ / G;
+    const auto rq = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(Q + (int64_t)(q0 + tok0) * qs + (int64_t)h * G * D), (short)0, 0x7fffffff, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int blk = wave + 4 * j, r = blk * RPB + lane / DC;
+      const int row = min(rt * kMassQ + r, rows - 1), tok = row / G;
+      const uint32_t off = (uint32_t)((tok - tok0) * (int)qs + (row - tok * G) * D + kv_chunk<D>(lane % DC, r) * 8) * 2;
+      buffer_load_lds16(rq, dst + blk * 512, off, 0);
     }
-  if (panel >= 0) c.mass[at] += sum;
+  };
+  float acc[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  const float* lp = lse + (int64_t)h * b.n_tokens * G + (int64_t)q0 * G;
+  gload(rt_lo, Int<0>{});
+  auto step = [&](int rt, auto buf) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (rt + 1 < rt_hi) gload(rt + 1, Int<1 - decltype(buf)::value>{});
+    const bf16* qb = decltype(buf)::value ? sq1 : sq0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 32 * u + lr, row = rt * kMassQ + r;
+      const bool there = row < rows;
+      const float off = there ? lp[row] : INFINITY;
+      const int qpos = ctx + min(row, rows - 1) / G;
+      f32x16 sc = f32x16{0.f};
+#pragma unroll
+      for (int t = 0; t < DS; ++t)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            kreg[t], *(const bf16x8*)&qb[r * D + kv_chunk<D>(2 * t + lg, r) * 8], sc, 0, 0, 0);
+      const bool edge = wkey + 31 > ctx + rt * kMassQ / G;  // some row may not see some key
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(sc[e], kf, -off));
+        const int key = wkey + (e & 3) + 8 * (e >> 2) + 4 * lg;
+        acc[e] += there && (!edge || key <= qpos) ? w : 0.f;
+      }
+    }
+  };
+  for (int rt = rt_lo; rt < rt_hi; rt += 2) {
+    step(rt, Int<0>{});
+    if (rt + 1 < rt_hi) step(rt + 1, Int<1>{});
+  }
+  float* mp = c.mass + kv8_row_at(c, Hkv, max(panel, 0), h, prow);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float sum = group_sum(acc[e], 32);
+    const int k = (e & 3) + 8 * (e >> 2) + 4 * lg;
+    if (lr == 0 && k < live) mp[k] += sum;
+  }
 }
 
+// Key-range splits: doubled while the workgroups still fit about one per CU and every
+// split keeps 8 tiles of the longest range.
+static int kv8_key_splits(const BatchDev& b, int n_q_heads, int n_kv_heads) {
+  const int64_t wgs = (int64_t)cdiv(b.n_tokens * (n_q_heads / n_kv_heads), kRows8) * n_kv_heads;
+  const int tiles = cdiv(b.max_ctx_len + b.max_q_len, kKeys8);
+  int sp = 1;
+  while (sp < kMaxSplitF8 && wgs * sp * 2 * 4 <= (int64_t)cu_count() * 5 && tiles >= 16 * sp) sp *= 2;
+  return sp;
+}
+
+static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+// Workspace: log-sum-exps of the packed rows (with mass), the splits' partials, the
+// single tokens' part.
+static size_t lse_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads) {
+  return c.mass && b.max_q_len > 1 ? round256((size_t)b.n_tokens * n_q_heads * 4) : 0;
+}
+// (a bound that never falls as tokens are added: splits > 1 leave room for 1.25 CUs' rows)
+static size_t part8_bytes(const BatchDev& b, int n_q_heads, int n_kv_heads, int head_dim) {
+  if (b.max_q_len < 2) return 0;
+  const int64_t rows = std::min<int64_t>((int64_t)kMaxSplitF8 * b.n_tokens * n_q_heads,
+                                         (int64_t)cu_count() * 5 / 4 * kRows8);
+  return round256((size_t)rows * (head_dim + 4) * 4);
+}
 size_t attn_kv8_workspace_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads, int n_kv_heads,
                                 int head_dim) {
-  const size_t lse = c.mass ? (size_t)b.n_tokens * n_q_heads * sizeof(float) : 0;
-  return (lse + 255) / 256 * 256 + attn_kv8_decode_bytes(b, c, n_q_heads, n_kv_heads, head_dim);
+  return lse_bytes(b, c, n_q_heads) + part8_bytes(b, n_q_heads, n_kv_heads, head_dim) +
+         attn_kv8_decode_bytes(b, c, n_q_heads, n_kv_heads, head_dim);
+}
+
+template <int D, bool FP8>
+static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv, const void* q,
+                             int64_t qs, void* out, char* ws, hipStream_t s) {
+  const int sp = kv8_key_splits(b, Hq, Hkv), G = Hq / Hkv;
+  float* lse = c.mass ? (float*)ws : nullptr;
+  float* part = (float*)(ws + lse_bytes(b, c, Hq));
+  const float scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
+  const int64_t wgs = (int64_t)cdiv(b.max_q_len * G, kRows8) * Hkv * b.n_seqs * sp;
+  if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
+  auto go = [&](auto kernel) {
+    kernel<<<(unsigned)wgs, 256, 0, s>>>(b, c, Hq, Hkv, (const bf16*)q, qs, (bf16*)out, lse, part, sp,
+                                         scale_log2e);
+    return hipGetLastError();
+  };
+  hipError_t e;
+  if (sp > 1) e = c.kv.table ? go(attn_kv8_kernel<D, FP8, true, true>) : go(attn_kv8_kernel<D, FP8, false, true>);
+  else e = c.kv.table ? go(attn_kv8_kernel<D, FP8, true, false>) : go(attn_kv8_kernel<D, FP8, false, false>);
+  if (e != hipSuccess) return e;
+  if (sp > 1) {
+    attn_kv8_fold_kernel<D><<<dim3(cdiv(b.max_q_len * G, 1024 / D), Hkv, b.n_seqs), 256, 0, s>>>(
+        b, c, Hq, Hkv, part, (bf16*)out, lse, sp);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (c.mass) {
+    attn_kv8_mass_kernel<D, FP8><<<dim3(cdiv(b.max_ctx_len + b.max_q_len, kMassKeys), Hkv, b.n_seqs), 256, 0, s>>>(
+        b, c, Hq, Hkv, (const bf16*)q, qs, lse, scale_log2e);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q_heads,
                            int n_kv_heads, int head_dim, const void* q, int64_t q_stride, void* out,
                            void* ws, hipStream_t s) {
   if (b.n_seqs == 0 || b.n_tokens == 0) return hipSuccess;
-  const float scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)head_dim));
-  float* lse = c.mass ? (float*)ws : nullptr;
-  const size_t lse_bytes = c.mass ? (size_t)b.n_tokens * n_q_heads * sizeof(float) : 0;
   if (b.max_q_len == 1 || (int64_t)b.n_seqs * b.max_q_len != b.n_tokens) {
-    const hipError_t e = launch_attn_kv8_decode(b, c, fp8, n_q_heads, n_kv_heads, head_dim, q, q_stride, out,
-                                                (float*)((char*)ws + (lse_bytes + 255) / 256 * 256), s);
+    float* own = (float*)((char*)ws + lse_bytes(b, c, n_q_heads) + part8_bytes(b, n_q_heads, n_kv_heads, head_dim));
+    const hipError_t e = launch_attn_kv8_decode(b, c, fp8, n_q_heads, n_kv_heads, head_dim, q, q_stride, out, own, s);
     if (e != hipSuccess || b.max_q_len == 1) return e;
   }
-  auto go = [&](auto attend, auto weigh) {
-    attend<<<dim3(b.n_tokens, n_q_heads), 256, 0, s>>>(b, c, n_q_heads, n_kv_heads, (const bf16*)q,
-                                                       q_stride, (bf16*)out, lse, scale_log2e);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !lse) return e;
-    const dim3 grid(cdiv(b.max_ctx_len + b.max_q_len, 256), n_kv_heads, b.n_seqs);
-    weigh<<<grid, 256, 0, s>>>(b, c, n_q_heads, n_kv_heads, (const bf16*)q, q_stride, lse, scale_log2e);
-    return hipGetLastError();
-  };
+  char* w = (char*)ws;
   if (head_dim == 128)
-    return fp8 ? go(attn_kv8_kernel<128, true>, mass_kv8_kernel<128, true>)
-               : go(attn_kv8_kernel<128, false>, mass_kv8_kernel<128, false>);
-  return fp8 ? go(attn_kv8_kernel<64, true>, mass_kv8_kernel<64, true>)
-             : go(attn_kv8_kernel<64, false>, mass_kv8_kernel<64, false>);
+    return fp8 ? run_flash8<128, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
+               : run_flash8<128, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
+  return fp8 ? run_flash8<64, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
+             : run_flash8<64, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
 }
 
 }  // namespace tri

@@ -49,18 +49,19 @@ __device__ __forceinline__ f16x8 codes_to_f16(uint32_t a, uint32_t b) {
   return u.v;
 }
 
-// A head's bf16 query values, 8 N of them in each of the lanes l, l ^ 16, l ^ 32, l ^ 48,
-// as float16 times a power of two that brings the largest to [2^14, 2^15); returns the
-// power of two that takes products back.  (A row that is not finite stays as it is.)
-template <int N>
+// A head's bf16 query values, 8 N of them in each of the lanes that differ in the bits
+// SHARE, as float16 times a power of two that brings the largest to [2^14, 2^15); returns
+// the power of two that takes products back.  (A row that is not finite stays as it is.)
+template <int SHARE, int N>
 __device__ __forceinline__ float q_to_f16(const Pack8 (&x)[N], f16x8 (&o)[N]) {
   uint32_t m = 0;
 #pragma unroll
   for (int j = 0; j < N; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(bf2f(x[j].e[e])) & 0x7fffffffu);
-  m = max(m, (uint32_t)__shfl_xor((int)m, 16, 64));
-  m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+#pragma unroll
+  for (int bit = 1; bit < 64; bit <<= 1)
+    if (SHARE & bit) m = max(m, (uint32_t)__shfl_xor((int)m, bit, 64));
   const int exp = (int)(m >> 23) - 127;  // (-127: zero or subnormal)
   const int up = m >= 0x7f800000u ? 0 : min(14 - exp, 126);
   const float f = __uint_as_float((uint32_t)(up + 127) << 23);
@@ -69,6 +70,14 @@ __device__ __forceinline__ float q_to_f16(const Pack8 (&x)[N], f16x8 (&o)[N]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[j][e] = (f16)(bf2f(x[j].e[e]) * f);
   return __uint_as_float((uint32_t)(127 - up) << 23);
+}
+
+// Largest of a lane's 16 scores.
+__device__ __forceinline__ float tree_max16(const f32x16& s) {
+  float m[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) m[i] = max3f(s[3 * i], s[3 * i + 1], s[3 * i + 2]);
+  return max3f(max3f(m[0], m[1], m[2]), max3f(m[3], m[4], s[15]), m[4]);
 }
 
 __device__ __forceinline__ float readlane_f(float v, int lane) {

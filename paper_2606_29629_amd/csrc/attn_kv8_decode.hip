@@ -178,7 +178,7 @@ __global__ __launch_bounds__(64, 2) void attn_kv8_decode_kernel(
     issue_k(Int<0>{}, 0);
     issue_v(1);
     issue_k(Int<1>{}, 1);
-    q_back = q_to_f16(x, qf);
+    q_back = q_to_f16<48>(x, qf);
   }
   const float score_scale = q_back * scale_log2e;
 

@@ -191,6 +191,7 @@ ATTEND = {
     "chunks": ([1, 0, 2], [0, 31, 64], [70, 33, 128]),
     "far chunk": ([0, 1], [1500, 3], [150, 2]),
     "mixed": ([3, 0, 1, 2], [600, 0, 33, 190], [1, 130, 0, 66]),
+    "farther chunk": ([1, 0], [4500, 4300], [19, 1]),
     "many": (list(range(24)), [37 * i % 300 for i in range(24)], [1 + (i % 5) * (i % 2) for i in range(24)]),
 }
 
