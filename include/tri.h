@@ -393,10 +393,16 @@ tri_status tri_kv8_attention(const tri_layer_config* cfg, const tri_kv8_cache* c
  * budget: a multiple of scale_rows, <= max_seq; n_first, n_recent >= 0 with n_first +
  * n_recent <= budget.  The rows kept are no longer in order of position: the stamps
  * tell it, and keys are cached rotated, so attention does not mind.  A skipped
- * sequence gets -1 throughout and new_len 0.                                      */
+ * sequence (also one whose lengths exceed the batch's host fields) gets -1 throughout
+ * and new_len 0.
+ * workspace: device, 256-byte aligned, of tri_kv8_select_workspace_size bytes (0, and NULL
+ * will do, unless max_ctx_len + max_q_len exceeds 16384 rows).                     */
+tri_status tri_kv8_select_workspace_size(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                                         const tri_batch* batch, int32_t budget, size_t* bytes);
 tri_status tri_kv8_select(const tri_layer_config* cfg, const tri_kv8_cache* cache,
                           const tri_batch* batch, int32_t budget, int32_t n_first,
-                          int32_t n_recent, int32_t* plan, int32_t* new_len, void* stream);
+                          int32_t n_recent, int32_t* plan, int32_t* new_len, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /* Eviction, second half: row r of every KV head takes what is in row plan[r] (codes,
  * mass, stamp), r < budget.  A scale block into which rows move takes the largest of

@@ -5,6 +5,7 @@ C ABI in include/tri.h); this package is its thin ctypes binding.
 """
 from ._lib import (DeviceBatch, KV8Cache, LayerConfig, PagedCache, Profile, RopeConfig, TriError, Work,
                    kv8_append, kv8_attention, kv8_attention_workspace_size, kv8_move, kv8_select,
+                   kv8_select_workspace_size,
                    kv_struct, kvcache_append,
                    layer_decode, layer_work, phase_intensity, profile_enable, profile_read,
                    work_dict, work_sum,
@@ -14,7 +15,7 @@ from ._lib import (DeviceBatch, KV8Cache, LayerConfig, PagedCache, Profile, Rope
 
 __all__ = ["DeviceBatch", "KV8Cache", "LayerConfig", "PagedCache", "Profile", "RopeConfig", "TriError",
            "Work", "kv8_append", "kv8_attention", "kv8_attention_workspace_size", "kv8_move",
-           "kv8_select", "kv_struct", "kvcache_append",
+           "kv8_select", "kv8_select_workspace_size", "kv_struct", "kvcache_append",
            "layer_decode", "layer_work", "phase_intensity", "work_dict", "work_sum",
            "layer_prefill", "lib", "linear", "linear_workspace_size", "profile_enable", "profile_read",
            "make_config", "make_rope", "moe_route", "rope", "status_string",

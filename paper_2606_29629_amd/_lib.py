@@ -122,8 +122,10 @@ _FUNCS = {
     "tri_kv8_attention": (ctypes.c_int, [ctypes.c_void_p] * 4
                           + [ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                              ctypes.c_void_p]),
+    "tri_kv8_select_workspace_size": (ctypes.c_int, [ctypes.c_void_p] * 3
+                                      + [ctypes.c_int32, ctypes.c_void_p]),
     "tri_kv8_select": (ctypes.c_int, [ctypes.c_void_p] * 3 + [ctypes.c_int32] * 3
-                       + [ctypes.c_void_p] * 3),
+                       + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p]),
     "tri_kv8_move": (ctypes.c_int, [ctypes.c_void_p] * 4 + [ctypes.c_int32, ctypes.c_void_p]),
 }
 
@@ -526,8 +528,16 @@ def kv8_attention(cfg, cache: KV8Cache, batch, q, out=None, workspace=None, stre
     return out, workspace
 
 
+def kv8_select_workspace_size(cfg, cache: KV8Cache, batch, budget: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().tri_kv8_select_workspace_size(
+        ctypes.byref(cfg), ctypes.byref(cache.struct()), ctypes.byref(batch.struct()), int(budget),
+        ctypes.byref(n)), "tri_kv8_select_workspace_size")
+    return n.value
+
+
 def kv8_select(cfg, cache: KV8Cache, batch, budget: int, n_first: int = 0, n_recent: int = 0,
-               plan=None, new_len=None, stream=None):
+               plan=None, new_len=None, workspace=None, stream=None):
     """Which rows of the batch's sequences (ctx_len + q_len each) stay within budget
     (tri_kv8_select); returns (plan [n_seqs, Hkv, budget], new_len [n_seqs]), int32."""
     import torch
@@ -539,8 +549,13 @@ def kv8_select(cfg, cache: KV8Cache, batch, budget: int, n_first: int = 0, n_rec
     _plan("kv8_select", plan, shape)
     if new_len.dtype != torch.int32 or new_len.numel() != batch.n_seqs or not new_len.is_contiguous():
         raise ValueError(f"kv8_select: new_len is a contiguous int32 [{batch.n_seqs}]")
-    _check(lib().tri_kv8_select(*_kv8("kv8_select", cfg, cache, batch, plan, new_len), int(budget),
-                                int(n_first), int(n_recent), _ptr(plan), _ptr(new_len),
+    args = _kv8("kv8_select", cfg, cache, batch, plan, new_len, workspace)
+    if workspace is None and batch.max_ctx_len + batch.max_q_len > 16384:  # (else none is needed)
+        workspace = torch.empty(kv8_select_workspace_size(cfg, cache, batch, budget),
+                                dtype=torch.uint8, device=plan.device)
+    _check(lib().tri_kv8_select(*args, int(budget), int(n_first), int(n_recent), _ptr(plan),
+                                _ptr(new_len), _ptr(workspace),
+                                0 if workspace is None else workspace.numel() * workspace.element_size(),
                                 _stream(stream)), "tri_kv8_select")
     return plan, new_len
 

@@ -226,8 +226,9 @@ size_t attn_kv8_workspace_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_head
 hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q_heads,
                            int n_kv_heads, int head_dim, const void* q, int64_t q_stride, void* out,
                            void* ws, hipStream_t s);
+size_t kv8_select_workspace_bytes(const BatchDev& b, int n_kv_heads, int budget);
 hipError_t launch_kv8_select(const BatchDev& b, const Kv8Dev& c, int n_kv_heads, int budget,
-                             int n_first, int n_recent, int32_t* plan, int32_t* new_len,
+                             int n_first, int n_recent, int32_t* plan, int32_t* new_len, void* ws,
                              hipStream_t s);
 hipError_t launch_kv8_move(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_kv_heads,
                            int head_dim, const int32_t* plan, int budget, hipStream_t s);

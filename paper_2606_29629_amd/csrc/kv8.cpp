@@ -83,6 +83,11 @@ tri_status check_group(const tri_layer_config* c) {
   return TRI_OK;
 }
 
+tri_status check_budget(const tri_kv8_cache* c, int32_t budget) {
+  if (budget <= 0 || budget % c->scale_rows != 0) return TRI_ERR_SHAPE;
+  return budget > c->max_seq ? TRI_ERR_RANGE : TRI_OK;
+}
+
 // Bytes from the first to the last element of T rows of `width`, `stride` apart.
 size_t extent(int64_t rows, int64_t width, int64_t stride, int size) {
   return (size_t)((rows - 1) * stride + width) * size;
@@ -219,19 +224,35 @@ tri_status tri_kv8_attention(const tri_layer_config* cfg, const tri_kv8_cache* c
   return TRI_OK;
 }
 
+tri_status tri_kv8_select_workspace_size(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                                         const tri_batch* b, int32_t budget, size_t* bytes) {
+  if (!bytes) return TRI_ERR_NULL;
+  tri_status st = check_call(cfg, cache, b);
+  if (st != TRI_OK) return st;
+  *bytes = 0;
+  if (b->n_seqs == 0) return TRI_OK;
+  if ((st = check_budget(cache, budget)) != TRI_OK) return st;
+  *bytes = kv8_select_workspace_bytes(batch_dev(b), cfg->n_kv_heads, budget);
+  return TRI_OK;
+}
+
 tri_status tri_kv8_select(const tri_layer_config* cfg, const tri_kv8_cache* cache,
                           const tri_batch* b, int32_t budget, int32_t n_first, int32_t n_recent,
-                          int32_t* plan, int32_t* new_len, void* stream) {
-  tri_status st = check_call(cfg, cache, b);
+                          int32_t* plan, int32_t* new_len, void* ws, size_t ws_bytes,
+                          void* stream) {
+  size_t need = 0;
+  tri_status st = tri_kv8_select_workspace_size(cfg, cache, b, budget, &need);
   if (st != TRI_OK) return st;
   if (b->n_seqs == 0) return TRI_OK;
   if (!plan || !cache->mass || !b->cu_q || !b->ctx_len || !b->slot) return TRI_ERR_NULL;
-  if (budget <= 0 || budget % cache->scale_rows != 0) return TRI_ERR_SHAPE;
-  if (budget > cache->max_seq) return TRI_ERR_RANGE;
   if (n_first < 0 || n_recent < 0 || (int64_t)n_first + n_recent > budget) return TRI_ERR_SHAPE;
   if ((uintptr_t)plan % 4 || (uintptr_t)new_len % 4) return TRI_ERR_ALIGN;
+  if (need > 0 && (!ws || ws_bytes < need)) return TRI_ERR_WORKSPACE;
+  if (need > 0 && ((uintptr_t)ws & (kAlign - 1)) != 0) return TRI_ERR_ALIGN;
+  const size_t plan_bytes = (size_t)b->n_seqs * cfg->n_kv_heads * budget * 4;
+  if (need > 0 && overlaps(ws, need, plan, plan_bytes)) return TRI_ERR_ALIAS;
   TRI_HIP(launch_kv8_select(batch_dev(b), kv8_dev(cache), cfg->n_kv_heads, budget, n_first, n_recent,
-                            plan, new_len, (hipStream_t)stream));
+                            plan, new_len, ws, (hipStream_t)stream));
   return TRI_OK;
 }
 
@@ -241,8 +262,7 @@ tri_status tri_kv8_move(const tri_layer_config* cfg, const tri_kv8_cache* cache,
   if (st != TRI_OK) return st;
   if (b->n_seqs == 0) return TRI_OK;
   if (!plan || !b->slot) return TRI_ERR_NULL;
-  if (budget <= 0 || budget % cache->scale_rows != 0) return TRI_ERR_SHAPE;
-  if (budget > cache->max_seq) return TRI_ERR_RANGE;
+  if ((st = check_budget(cache, budget)) != TRI_OK) return st;
   if ((uintptr_t)plan % 4) return TRI_ERR_ALIGN;
   TRI_HIP(launch_kv8_move(batch_dev(b), kv8_dev(cache), cache->format == TRI_KV8_E4M3,
                           cfg->n_kv_heads, cfg->head_dim, plan, budget, (hipStream_t)stream));

@@ -120,154 +120,435 @@ hipError_t launch_kv8_append(const BatchDev& b, const Kv8Dev& c, bool fp8, int n
              : go(kv8_append_kernel<64, false, 4>, kv8_append_kernel<64, false, 1>);
 }
 
-// Select.  One workgroup per (head, sequence).  A row's key is its mass as an unsigned
-// integer of the same order (protected rows above all, NaN below all); the budget-th
-// largest key is found by three histograms of 11, 11 and 10 bits in LDS (integer
-// counts: no order changes them), and one pass in row order then knows of every row,
-// from the counts of greater and equal keys before it, whether it stays and, of rows
-// evicted below budget and kept past it, the how-manieth it is.  The latter's rows are
-// paired through a list in LDS, kSelList at a time.
-constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
-constexpr int kSelBins = 2048, kSelList = 8192;
+// Select.  A row's key is its mass as an unsigned integer of the same order (protected
+// rows above all, NaN below all).  The budget-th largest key T of a (sequence, head) is
+// found by histograms of its upper 11, next 11 and last 10 bits (integer counts: no order
+// changes them); then of every row, from the counts of greater and equal keys before it,
+// it is known whether it stays and, of rows evicted below budget and of rows kept past it,
+// the how-manieth it is, which pairs them.  The work is a few operations a row, eight bytes
+// read: a chain of short dependent steps bounds it, not bytes.
+//
+// Up to kSelOneRows rows one workgroup of 1024 threads does it all, K neighbouring rows a
+// thread with their keys in registers (4352 rows: 64 x 4 heads in %SHORT%).
+// Longer sequences take a workgroup per kSelChunk rows and one launch per step.
+constexpr int kSelThreads = 1024;
+constexpr int kSelOneRows = 16 * kSelThreads;
+constexpr int kSelBins = 2048;
+constexpr int kSelChunk = 2048;  // rows of a workgroup of 256, eight a thread
+constexpr int kSelK = 8;
 
+// The sequence's rows; 0 where it is skipped (also if past the batch's host fields, which
+// the buffers are sized by).
+__device__ __forceinline__ int select_rows(const BatchDev& b, const Kv8Dev& c, int s, int& sl) {
+  int q0, nq, ctx;
+  const bool ok = kv8_seq(b, c, s, q0, nq, ctx, sl);
+  return ok && ctx <= b.max_ctx_len && nq <= b.max_q_len ? ctx + nq : 0;
+}
+
+// Mass and stamp of K neighbouring rows r .. (K divides the page; rows past n: 0).
+template <int K>
+__device__ __forceinline__ void select_load(const Kv8Dev& c, int Hkv, int h, int sl, int r, int n,
+                                            float (&m)[K], int (&a)[K]) {
+  int prow = 0;
+  const int panel = r < n ? kv_panel(c.kv, sl, r, prow) : -1;
+  const int64_t at = kv8_row_at(c, Hkv, max(panel, 0), h, prow);
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const bool there = panel >= 0 && r + i < n;
+    m[i] = there ? c.mass[at + i] : 0.f;
+    a[i] = there && c.stamp ? c.stamp[at + i] : r + i;
+  }
+}
+
+// A stamp as an unsigned integer of the same order.
+__device__ __forceinline__ uint32_t stamp_key(int a) { return (uint32_t)a ^ 0x80000000u; }
+
+__device__ __forceinline__ uint32_t select_key(float m, int age, uint32_t newest, int n_first,
+                                               int n_recent) {
+  const int64_t last_old = (int64_t)(int)(newest ^ 0x80000000u) - n_recent;
+  if (age < n_first || age > last_old) return 0xffffffffu;
+  if (m != m) return 0u;
+  const uint32_t u = __float_as_uint(m + 0.f);  // (-0 becomes 0)
+  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+}
+
+constexpr int select_shift(int pass) { return pass == 0 ? 21 : (pass == 1 ? 10 : 0); }
+constexpr int select_bins(int pass) { return pass == 2 ? 1024 : 2048; }
+constexpr int kSelHist = 2048 + 2048 + 1024;  // the three histograms of a head
+constexpr int select_hist_at(int pass) { return pass * 2048; }
+
+// The bin in which the counts from the top reach `need`, and the count above it.  W waves;
+// `red` holds W words, `found` two; every thread gets the answer.
+template <int W>
+__device__ __forceinline__ void select_bin(const uint32_t* hist, int bins, int need, uint32_t* red,
+                                           uint32_t* found, int& bin, int& above) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = bins / (64 * W);
+  uint32_t mine = 0;
+  for (int i = 0; i < per; ++i) mine += hist[bins - 1 - (tid * per + i)];
+  uint32_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t v = (uint32_t)__shfl_up((int)upto, o, 64);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 63) red[wave] = upto;
+  __syncthreads();
+  uint32_t over = upto - mine;
+#pragma unroll
+  for (int w = 0; w < W; ++w) over += w < wave ? red[w] : 0u;
+  for (int i = 0; i < per; ++i) {
+    const int at = bins - 1 - (tid * per + i);
+    const uint32_t cnt = hist[at];
+    if (over < (uint32_t)need && over + cnt >= (uint32_t)need) {
+      found[0] = (uint32_t)at;
+      found[1] = over;
+    }
+    over += cnt;
+  }
+  __syncthreads();
+  bin = (int)found[0];
+  above = (int)found[1];
+}
+
+// Exclusive prefixes of two counts over the workgroup, and their totals.
+template <int W>
+__device__ __forceinline__ void block_prefix2(int a, int e, int& pa, int& pe, int& ta, int& te,
+                                              int (*red)[2]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int ua = a, ue = e;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(ua, o, 64), y = __shfl_up(ue, o, 64);
+    if (lane >= o) {
+      ua += x;
+      ue += y;
+    }
+  }
+  if (lane == 63) {
+    red[wave][0] = ua;
+    red[wave][1] = ue;
+  }
+  __syncthreads();
+  pa = ua - a;
+  pe = ue - e;
+  ta = te = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const int x = red[w][0], y = red[w][1];
+    if (w < wave) {
+      pa += x;
+      pe += y;
+    }
+    ta += x;
+    te += y;
+  }
+}
+
+template <int K>
 __global__ __launch_bounds__(kSelThreads) void kv8_select_kernel(BatchDev b, Kv8Dev c, int Hkv,
                                                                  int budget, int n_first,
                                                                  int n_recent,
                                                                  int32_t* __restrict__ plan,
                                                                  int32_t* __restrict__ new_len) {
-  __shared__ uint32_t hist[kSelBins];
-  __shared__ int list[kSelList];
-  __shared__ uint32_t red[kSelWaves];
-  __shared__ int wave_gt[kSelWaves], wave_eq[kSelWaves];
-  __shared__ uint32_t found[2];
-  const int s = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
-  const int lane = tid & 63, wave = tid >> 6;
-  int q0, nq, ctx, sl;
-  const bool ok = kv8_seq(b, c, s, q0, nq, ctx, sl);
-  const int n = ok ? ctx + nq : 0;
+  constexpr int W = kSelThreads / 64;
+  __shared__ uint32_t hist[kSelBins], red[W], found[2];
+  __shared__ int sums[W][2], kept_low_at, list[K * kSelThreads / 2];  // (pairs: half of the rows at most)
+  const int s = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, r0 = tid * K;
+  int sl;
+  const int n = select_rows(b, c, s, sl);
   int32_t* out = plan + ((int64_t)s * Hkv + h) * budget;
   if (h == 0 && tid == 0 && new_len) new_len[s] = min(n, budget);
   if (n <= budget) {
     for (int r = tid; r < budget; r += kSelThreads) out[r] = r < n ? r : -1;
     return;
   }
-  auto place = [&](int r) {  // index of the row's mass and stamp; -1: no page
-    int prow;
-    const int panel = kv_panel(c.kv, sl, r, prow);
-    return panel < 0 ? (int64_t)-1 : kv8_row_at(c, Hkv, panel, h, prow);
-  };
-  auto age = [&](int r, int64_t at) { return c.stamp && at >= 0 ? c.stamp[at] : r; };
-  uint32_t newest = 0;  // (stamps as unsigned integers of the same order)
-  for (int r = tid; r < n; r += kSelThreads)
-    newest = max(newest, (uint32_t)age(r, place(r)) ^ 0x80000000u);
-  newest = block_max<kSelWaves>(newest, red);
-  const int64_t last_old = (int64_t)(int)(newest ^ 0x80000000u) - n_recent;  // stamps past it are recent
-  auto key = [&](int r) -> uint32_t {
-    const int64_t at = place(r);
-    const int a = age(r, at);
-    if (a < n_first || a > last_old) return 0xffffffffu;
-    const float m = at >= 0 ? c.mass[at] + 0.f : 0.f;  // (-0 becomes 0)
-    if (m != m) return 0u;
-    const uint32_t u = __float_as_uint(m);
-    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
-  };
-  // The budget-th largest key T, and how many rows equal to T stay.
-  uint32_t T = 0, mask = 0;
+  uint32_t key[K];
+  {
+    float m[K];
+    int a[K];
+    select_load<K>(c, Hkv, h, sl, r0, n, m, a);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < K; ++i) top = max(top, r0 + i < n ? stamp_key(a[i]) : 0u);
+    top = block_max<W>(top, red);
+#pragma unroll
+    for (int i = 0; i < K; ++i) key[i] = select_key(m[i], a[i], top, n_first, n_recent);
+  }
+  uint32_t T = 0;
   int need = budget;
+#pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048;
+    const int shift = select_shift(pass), bins = select_bins(pass);
+    const uint32_t mask = pass == 0 ? 0u : ~0u << select_shift(pass - 1);
     for (int i = tid; i < bins; i += kSelThreads) hist[i] = 0;
     __syncthreads();
-    for (int r = tid; r < n; r += kSelThreads) {
-      const uint32_t k = key(r);
-      if ((k & mask) == T) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
-    }
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (r0 + i < n && (key[i] & mask) == T) atomicAdd(&hist[(key[i] >> shift) & (bins - 1)], 1u);
     __syncthreads();
-    // Rows in greater bins, by thread: bins per thread (descending), a scan over waves.
-    const int per = bins / kSelThreads;
-    uint32_t mine = 0;
-    for (int i = 0; i < per; ++i) mine += hist[bins - 1 - (tid * per + i)];
-    uint32_t upto = mine;
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t v = (uint32_t)__shfl_up((int)upto, o, 64);
-      if (lane >= o) upto += v;
-    }
-    if (lane == 63) red[wave] = upto;
-    __syncthreads();
-    uint32_t above = upto - mine;
-    for (int w = 0; w < wave; ++w) above += red[w];
-    for (int i = 0; i < per; ++i) {
-      const int bin = bins - 1 - (tid * per + i);
-      const uint32_t cnt = hist[bin];
-      if (above < (uint32_t)need && above + cnt >= (uint32_t)need) {
-        found[0] = (uint32_t)bin;
-        found[1] = above;
-      }
-      above += cnt;
-    }
-    __syncthreads();
-    T |= found[0] << shift;
-    mask |= (uint32_t)(bins - 1) << shift;
-    need -= (int)found[1];
-    __syncthreads();
+    int bin, above;
+    select_bin<W>(hist, bins, need, red, found, bin, above);
+    T |= (uint32_t)bin << shift;
+    need -= above;
   }
-  // In row order: keys greater than and equal to T before each row.
-  int gt0 = 0, eq0 = 0;  // before the tile
-  auto scan = [&](bool gt, bool eq, int& ngt, int& neq) {
-    const uint64_t bg = __builtin_amdgcn_ballot_w64(gt), be = __builtin_amdgcn_ballot_w64(eq);
-    const uint64_t below = (1ull << lane) - 1;
-    if (lane == 0) {
-      wave_gt[wave] = __builtin_popcountll(bg);
-      wave_eq[wave] = __builtin_popcountll(be);
-    }
-    __syncthreads();
-    ngt = gt0 + __builtin_popcountll(bg & below);
-    neq = eq0 + __builtin_popcountll(be & below);
-    for (int w = 0; w < kSelWaves; ++w) {
-      const int g = wave_gt[w], e = wave_eq[w];
-      if (w < wave) { ngt += g; neq += e; }
-      gt0 += g;
-      eq0 += e;
-    }
-    __syncthreads();
-  };
-  for (int r0 = 0; r0 < budget; r0 += kSelThreads) {
-    const int r = r0 + tid;
-    const uint32_t k = r < budget ? key(r) : 0;
-    const bool gt = r < budget && k > T, eq = r < budget && k == T;
-    int ngt, neq;
-    scan(gt, eq, ngt, neq);
-    // kept before r: the greater ones and the first `need` equal ones
-    if (r < budget) out[r] = gt || (eq && neq < need) ? r : -2 - (r - (ngt + min(neq, need)));
+  // Kept before a row: the greater keys and the first `need` equal ones.
+  int gt = 0, eq = 0;
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    gt += r0 + i < n && key[i] > T;
+    eq += r0 + i < n && key[i] == T;
   }
-  const int kept_low = gt0 + min(eq0, need), gt_low = gt0, eq_low = eq0;
-  for (int base = 0; base < budget - kept_low; base += kSelList) {
-    gt0 = gt_low;
-    eq0 = eq_low;
-    for (int r0 = budget; r0 < n; r0 += kSelThreads) {
-      const int r = r0 + tid;
-      const uint32_t k = r < n ? key(r) : 0;
-      const bool gt = r < n && k > T, eq = r < n && k == T;
-      int ngt, neq;
-      scan(gt, eq, ngt, neq);
-      const int j = ngt + min(neq, need) - kept_low - base;
-      if ((gt || (eq && neq < need)) && j >= 0 && j < kSelList) list[j] = r;
-    }
-    __syncthreads();
-    for (int r = tid; r < budget; r += kSelThreads) {  // (a thread reads what it wrote)
-      const int v = out[r], j = -2 - v - base;
-      if (v <= -2 && j >= 0 && j < kSelList) out[r] = list[j];
-    }
-    __syncthreads();
+  int ngt, neq, all_gt, all_eq;
+  block_prefix2<W>(gt, eq, ngt, neq, all_gt, all_eq, sums);
+  int place[K];  // kept rows before each row
+  bool keep[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const bool there = r0 + i < n, more = there && key[i] > T, same = there && key[i] == T;
+    place[i] = ngt + min(neq, need);
+    keep[i] = more || (same && neq < need);
+    if (r0 + i == budget) kept_low_at = place[i];
+    ngt += more;
+    neq += same;
+  }
+  __syncthreads();
+  const int kept_low = kept_low_at;
+#pragma unroll
+  for (int i = 0; i < K; ++i)
+    if (keep[i] && r0 + i >= budget) list[place[i] - kept_low] = r0 + i;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const int r = r0 + i;
+    if (r < budget) out[r] = keep[i] ? r : list[r - place[i]];
   }
 }
 
+// The same in steps over chunks (grid: chunk, head, sequence).  Per (sequence, head) in the
+// workspace: every row's key, the histograms, and of every chunk its newest stamp and its
+// counts of greater and equal keys; the rows that move, in order.
+struct SelectWs {
+  uint32_t *key, *hist, *newest;
+  int32_t *count, *list;
+  int chunks, list_rows;
+  __device__ uint32_t* keys_of(int64_t p) const { return key + p * chunks * kSelChunk; }
+  __device__ uint32_t* hist_of(int64_t p, int pass) const { return hist + p * kSelHist + select_hist_at(pass); }
+};
+
+__global__ __launch_bounds__(256) void select_newest_kernel(BatchDev b, Kv8Dev c, int Hkv, int budget,
+                                                            SelectWs w) {
+  __shared__ uint32_t red[4];
+  const int s = blockIdx.z, h = blockIdx.y, r0 = blockIdx.x * kSelChunk + (int)threadIdx.x * kSelK;
+  const int64_t pair = (int64_t)s * Hkv + h;
+  int sl;
+  const int n = select_rows(b, c, s, sl);
+  if (n <= budget) return;
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < kSelHist; i += 256) w.hist[pair * kSelHist + i] = 0;
+  uint32_t top = 0;
+  if (c.stamp) {
+    float m[kSelK];
+    int a[kSelK];
+    select_load<kSelK>(c, Hkv, h, sl, r0, n, m, a);
+#pragma unroll
+    for (int i = 0; i < kSelK; ++i) top = max(top, r0 + i < n ? stamp_key(a[i]) : 0u);
+    top = block_max<4>(top, red);
+  } else {
+    top = stamp_key(n - 1);
+  }
+  if (threadIdx.x == 0) w.newest[pair * w.chunks + blockIdx.x] = top;
+}
+
+// T's digits and the equal keys still needed after the first `passes` histograms.
+template <int PASSES>
+__device__ __forceinline__ uint32_t select_digits(const SelectWs& w, int64_t pair, int budget,
+                                                  uint32_t* red, uint32_t* found, int& need) {
+  uint32_t T = 0;
+  need = budget;
+#pragma unroll
+  for (int pass = 0; pass < PASSES; ++pass) {
+    int bin, above;
+    __syncthreads();
+    select_bin<4>(w.hist_of(pair, pass), select_bins(pass), need, red, found, bin, above);
+    T |= (uint32_t)bin << select_shift(pass);
+    need -= above;
+  }
+  return T;
+}
+
+template <int PASS>
+__global__ __launch_bounds__(256) void select_hist_kernel(BatchDev b, Kv8Dev c, int Hkv, int budget,
+                                                          int n_first, int n_recent, SelectWs w) {
+  constexpr int BINS = select_bins(PASS), SHIFT = select_shift(PASS);
+  __shared__ uint32_t hist[BINS], red[4], found[2];
+  const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+  const int r0 = blockIdx.x * kSelChunk + tid * kSelK;
+  const int64_t pair = (int64_t)s * Hkv + h;
+  int sl;
+  const int n = select_rows(b, c, s, sl);
+  if (n <= budget || (int)blockIdx.x * kSelChunk >= n) return;
+  for (int i = tid; i < BINS; i += 256) hist[i] = 0;
+  uint32_t key[kSelK];
+  u32x4* kp = (u32x4*)(w.keys_of(pair) + r0);
+  uint32_t T = 0, mask = 0;
+  if constexpr (PASS == 0) {
+    float m[kSelK];
+    int a[kSelK];
+    select_load<kSelK>(c, Hkv, h, sl, r0, n, m, a);
+    uint32_t top = 0;
+    for (int i = tid; i < cdiv(n, kSelChunk); i += 256) top = max(top, w.newest[pair * w.chunks + i]);
+    top = block_max<4>(top, red);
+#pragma unroll
+    for (int i = 0; i < kSelK; ++i) key[i] = select_key(m[i], a[i], top, n_first, n_recent);
+    kp[0] = u32x4{key[0], key[1], key[2], key[3]};
+    kp[1] = u32x4{key[4], key[5], key[6], key[7]};
+  } else {
+    const u32x4 x = kp[0], y = kp[1];
+#pragma unroll
+    for (int i = 0; i < kSelK; ++i) key[i] = i < 4 ? x[i] : y[i - 4];
+    int need;
+    T = select_digits<PASS>(w, pair, budget, red, found, need);
+    mask = ~0u << select_shift(PASS - 1);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSelK; ++i)
+    if (r0 + i < n && (key[i] & mask) == T) atomicAdd(&hist[(key[i] >> SHIFT) & (BINS - 1)], 1u);
+  __syncthreads();
+  uint32_t* all = w.hist_of(pair, PASS);
+  for (int i = tid; i < BINS; i += 256)
+    if (hist[i]) atomicAdd(&all[i], hist[i]);
+}
+
+// ASSIGN false: the chunk's counts; true: what becomes of each of its rows.
+template <bool ASSIGN>
+__global__ __launch_bounds__(256) void select_place_kernel(BatchDev b, Kv8Dev c, int Hkv, int budget,
+                                                           SelectWs w, int32_t* __restrict__ plan,
+                                                           int32_t* __restrict__ new_len) {
+  __shared__ uint32_t red[4], found[2];
+  __shared__ int sums[4][2], total[2][4][2];
+  const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, chunk = blockIdx.x;
+  const int r0 = chunk * kSelChunk + tid * kSelK;
+  const int64_t pair = (int64_t)s * Hkv + h;
+  int sl;
+  const int n = select_rows(b, c, s, sl);
+  int32_t* out = plan + pair * budget;
+  if (ASSIGN && h == 0 && chunk == 0 && tid == 0 && new_len) new_len[s] = min(n, budget);
+  if (n <= budget) {
+    if (ASSIGN)
+      for (int r = chunk * kSelChunk + tid; r < min(budget, (chunk + 1) * kSelChunk); r += 256)
+        out[r] = r < n ? r : -1;
+    return;
+  }
+  if (chunk * kSelChunk >= n) return;
+  const u32x4* kp = (const u32x4*)(w.keys_of(pair) + r0);
+  const u32x4 x = kp[0], y = kp[1];
+  int need;
+  const uint32_t T = select_digits<3>(w, pair, budget, red, found, need);
+  uint32_t key[kSelK];
+  int gt = 0, eq = 0, gt_low = 0, eq_low = 0;  // (low: rows below budget)
+#pragma unroll
+  for (int i = 0; i < kSelK; ++i) {
+    key[i] = i < 4 ? x[i] : y[i - 4];
+    const int g = r0 + i < n && key[i] > T, e = r0 + i < n && key[i] == T;
+    gt += g;
+    eq += e;
+    gt_low += r0 + i < budget ? g : 0;
+    eq_low += r0 + i < budget ? e : 0;
+  }
+  int ngt, neq, all_gt, all_eq;
+  block_prefix2<4>(gt, eq, ngt, neq, all_gt, all_eq, sums);
+  int32_t* counts = w.count + pair * w.chunks * 4;
+  if constexpr (!ASSIGN) {
+    __syncthreads();
+    int a, e, low_gt, low_eq;
+    block_prefix2<4>(gt_low, eq_low, a, e, low_gt, low_eq, sums);
+    if (tid == 0) *(int4*)(counts + 4 * chunk) = make_int4(all_gt, all_eq, low_gt, low_eq);
+    return;
+  } else {
+    // counts of the chunks before this one, and of all rows below budget
+    int before_gt = 0, before_eq = 0, low_gt = 0, low_eq = 0;
+    for (int i = tid; i < cdiv(n, kSelChunk); i += 256) {
+      const int4 v = *(const int4*)(counts + 4 * i);
+      before_gt += i < chunk ? v.x : 0;
+      before_eq += i < chunk ? v.y : 0;
+      low_gt += v.z;
+      low_eq += v.w;
+    }
+    int a, e, g0, e0, g1, e1;
+    block_prefix2<4>(before_gt, before_eq, a, e, g0, e0, total[0]);
+    block_prefix2<4>(low_gt, low_eq, a, e, g1, e1, total[1]);
+    const int kept_low = g1 + min(e1, need);
+    ngt += g0;
+    neq += e0;
+#pragma unroll
+    for (int i = 0; i < kSelK; ++i) {
+      const int r = r0 + i;
+      const bool same = key[i] == T, keep = r < n && (key[i] > T || (same && neq < need));
+      const int place = ngt + min(neq, need);
+      ngt += key[i] > T;
+      neq += same;
+      if (r < budget) out[r] = keep ? r : -2 - (r - place);
+      else if (keep) w.list[pair * w.list_rows + place - kept_low] = r;
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void select_pair_kernel(int budget, SelectWs w,
+                                                          int32_t* __restrict__ plan) {
+  const int64_t pair = (int64_t)blockIdx.z * gridDim.y + blockIdx.y;
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r >= budget) return;
+  int32_t* out = plan + pair * budget + r;
+  const int v = *out;
+  if (v <= -2) *out = w.list[pair * w.list_rows + (-2 - v)];
+}
+
+static int select_most(const BatchDev& b) {
+  return (int)std::min<int64_t>((int64_t)b.max_ctx_len + b.max_q_len, 0x7fffffff - kSelChunk);
+}
+size_t kv8_select_workspace_bytes(const BatchDev& b, int n_kv_heads, int budget) {
+  const int most = select_most(b);
+  if (most <= kSelOneRows || most <= budget) return 0;
+  const size_t pairs = (size_t)b.n_seqs * n_kv_heads, chunks = cdiv(most, kSelChunk);
+  const size_t list = std::min(budget, most - budget);
+  return 4 * pairs * (chunks * kSelChunk + kSelHist + chunks * 5 + (list + 3) / 4 * 4) + 64;
+}
+
 hipError_t launch_kv8_select(const BatchDev& b, const Kv8Dev& c, int n_kv_heads, int budget,
-                             int n_first, int n_recent, int32_t* plan, int32_t* new_len,
+                             int n_first, int n_recent, int32_t* plan, int32_t* new_len, void* ws,
                              hipStream_t s) {
   if (b.n_seqs == 0) return hipSuccess;
-  kv8_select_kernel<<<dim3(n_kv_heads, b.n_seqs), kSelThreads, 0, s>>>(b, c, n_kv_heads, budget,
-                                                                      n_first, n_recent, plan, new_len);
+  const int most = select_most(b);
+  if (most <= kSelOneRows || most <= budget) {
+    auto go = [&](auto kernel) {
+      kernel<<<dim3(n_kv_heads, b.n_seqs), kSelThreads, 0, s>>>(b, c, n_kv_heads, budget, n_first,
+                                                               n_recent, plan, new_len);
+      return hipGetLastError();
+    };
+    if (most <= 2 * kSelThreads || most <= budget) return go(kv8_select_kernel<2>);
+    if (most <= 4 * kSelThreads) return go(kv8_select_kernel<4>);
+    if (most <= 8 * kSelThreads) return go(kv8_select_kernel<8>);
+    return go(kv8_select_kernel<16>);
+  }
+  SelectWs w{};
+  const size_t pairs = (size_t)b.n_seqs * n_kv_heads;
+  w.chunks = cdiv(most, kSelChunk);
+  w.list_rows = std::min(budget, most - budget);
+  w.key = (uint32_t*)ws;
+  w.count = (int32_t*)(w.key + pairs * w.chunks * kSelChunk);
+  w.hist = (uint32_t*)(w.count + pairs * w.chunks * 4);
+  w.newest = w.hist + pairs * kSelHist;
+  w.list = (int32_t*)(w.newest + pairs * w.chunks);
+  const dim3 grid(w.chunks, n_kv_heads, b.n_seqs);
+  select_newest_kernel<<<grid, 256, 0, s>>>(b, c, n_kv_heads, budget, w);
+  select_hist_kernel<0><<<grid, 256, 0, s>>>(b, c, n_kv_heads, budget, n_first, n_recent, w);
+  select_hist_kernel<1><<<grid, 256, 0, s>>>(b, c, n_kv_heads, budget, n_first, n_recent, w);
+  select_hist_kernel<2><<<grid, 256, 0, s>>>(b, c, n_kv_heads, budget, n_first, n_recent, w);
+  select_place_kernel<false><<<grid, 256, 0, s>>>(b, c, n_kv_heads, budget, w, plan, new_len);
+  select_place_kernel<true><<<grid, 256, 0, s>>>(b, c, n_kv_heads, budget, w, plan, new_len);
+  select_pair_kernel<<<dim3(cdiv(budget, 256), n_kv_heads, b.n_seqs), 256, 0, s>>>(budget, w, plan);
   return hipGetLastError();
 }
 

@@ -344,6 +344,8 @@ EVICT = {
     "short": ([1, 0], [30, 63], [1, 1], 64, 4, 16),
     "cut": ([0, 2, 1], [200, 127, 255], [1, 0, 1], 128, 4, 32),
     "long": ([0, 1], [4999, 900], [1, 100], 2048, 8, 100),
+    "longest": ([1, 0, 2], [30001, 16384, 600], [1, 1, 1], 4096, 4, 500),
+    "half of long": ([0], [20479], [1], 10240, 0, 10240),
     "nearly all": ([0], [1091], [5], 1088, 0, 0),
     "bad slot": ([5, 0, -1], [100, 200, 3], [1, 1, 1], 32, 1, 31),
 }
@@ -357,6 +359,8 @@ def test_select_and_move(name, page, stamp):
     for d, fmt in ((64, "int8"), (128, "e4m3")):
         cfg = config(4, 2, d)
         max_seq = -(-max(c + n for c, n in zip(ctx, q)) // 64) * 64
+        if max_seq > 10000 and d == 128:
+            continue   # (the host's reference takes its time)
         cache = make_cache(cfg, 3, max_seq, fmt, 32, page, seed=budget, stamp=stamp)
         if stamp:   # positions in any order, as after an eviction
             cache.stamp.copy_(cache.stamp % (2 * max_seq))
@@ -374,7 +378,7 @@ def test_select_and_move(name, page, stamp):
         same_cache(cache, ref)
 
 
-@pytest.mark.parametrize("rows", [129, 2300])
+@pytest.mark.parametrize("rows", [129, 2300, 5000, 9000, 17000])
 def test_select_ties_and_strange_weights(rows):
     """Equal weights go to the lower rows; NaN last, infinities and -0 in their order."""
     cfg = config(2, 2, 64)

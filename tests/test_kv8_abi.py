@@ -87,9 +87,10 @@ def attend(lib, c=None, kv=None, b=None, q=FAKE + (8 << 20), stride=256, out=FAK
 
 
 def select(lib, c=None, kv=None, b=None, budget=64, first=4, recent=16, plan=FAKE + (8 << 20),
-           new_len=FAKE + (9 << 20)):
+           new_len=FAKE + (9 << 20), ws=FAKE + (10 << 20), ws_bytes=1 << 30):
     return lib.tri_kv8_select(ctypes.byref(c or cfg()), ctypes.byref(kv or cache()),
-                              ctypes.byref(b or batch()), budget, first, recent, plan, new_len, None)
+                              ctypes.byref(b or batch()), budget, first, recent, plan, new_len, ws,
+                              ws_bytes, None)
 
 
 def move(lib, c=None, kv=None, b=None, plan=FAKE + (8 << 20), budget=64):
@@ -160,6 +161,18 @@ def test_eviction_refusals(lib):
     assert select(lib, first=40, recent=40) == T.TRI_ERR_SHAPE
     assert select(lib, plan=FAKE + 2) == T.TRI_ERR_ALIGN
     assert move(lib, plan=None) == T.TRI_ERR_NULL
+    long = dict(kv=cache(max_seq=1 << 17), b=batch(max_ctx=100000))       # a workspace is needed
+    assert select(lib, ws=None, **long) == T.TRI_ERR_WORKSPACE
+    assert select(lib, ws_bytes=4096, **long) == T.TRI_ERR_WORKSPACE
+    assert select(lib, ws=FAKE + 16, **long) == T.TRI_ERR_ALIGN
+    assert select(lib, ws=FAKE + (8 << 20), **long) == T.TRI_ERR_ALIAS    # the plan's own memory
+    n = ctypes.c_size_t(1)
+    for rows, some in ((16380, False), (16381, True)):                    # and max_q_len 4
+        b = batch(max_ctx=rows)
+        kv = cache(max_seq=1 << 17)
+        assert lib.tri_kv8_select_workspace_size(ctypes.byref(cfg()), ctypes.byref(kv),
+                                                 ctypes.byref(b), 64, ctypes.byref(n)) == T.TRI_OK
+        assert (n.value > 0) == some
 
 
 def rope(lib, c=None, x=FAKE, xs=512, y=FAKE + (1 << 20), ys=512, pos=FAKE + (2 << 20), tokens=4,
