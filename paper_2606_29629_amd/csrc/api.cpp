@@ -6,11 +6,11 @@
 #include <string.h>
 
 #include <algorithm>
-#include <mutex>
 
 #include "../../include/tri.h"
 #include "host.hpp"
 #include "kernels.hpp"
+#include "side.hpp"
 #include "stage.hpp"
 
 using namespace tri;
@@ -228,63 +228,6 @@ Layout layout_of(const tri_layer_config* c, const tri_batch* b) {
 
 template <typename T>
 T* at(void* ws, size_t off) { return (T*)((char*)ws + off); }
-
-// A second stream per device, on which a mixed batch's split-KV attention
-// (the single-token sequences) runs beside the flash attention of its
-// multi-token sequences: both read the projected q and the cache, and they
-// write disjoint output rows and disjoint partials.  Created on first use
-// (default priority, non-blocking); the fork and join events are recorded and
-// waited on under the device's lock, so concurrent callers cannot pair one
-// caller's record with another's wait.
-struct SideStream {
-  std::mutex mu;
-  hipStream_t s = nullptr;
-  hipEvent_t fork = nullptr, join = nullptr;
-  bool failed = false;  // creation failed once (e.g. under graph capture): run serially
-};
-constexpr int kMaxSideDevices = 64;
-// The side stream of the current device, or nullptr (run on the caller's
-// stream) when the caller's stream belongs to another device.
-SideStream* side_stream(hipStream_t caller) {
-  static SideStream ss[kMaxSideDevices];
-  int dev = -1, sdev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxSideDevices) return nullptr;
-  if (caller && (hipStreamGetDevice(caller, &sdev) != hipSuccess || sdev != dev)) {
-    (void)hipGetLastError();
-    return nullptr;
-  }
-  return &ss[dev];
-}
-// With the device's lock held: makes sure the stream and events exist; false
-// means "run on the caller's stream".  No stream is created while the
-// caller's stream is being captured into a graph (creating one could
-// invalidate the capture); an existing side stream joins the capture through
-// the fork and join events.
-bool side_ready(SideStream& x, hipStream_t caller) {
-  if (x.s) return true;
-  if (x.failed) return false;
-  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(caller, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) {
-    (void)hipGetLastError();
-    return false;
-  }
-  hipStream_t st = nullptr;
-  hipEvent_t f = nullptr, j = nullptr;
-  if (hipStreamCreateWithFlags(&st, hipStreamNonBlocking) == hipSuccess &&
-      hipEventCreateWithFlags(&f, hipEventDisableTiming) == hipSuccess &&
-      hipEventCreateWithFlags(&j, hipEventDisableTiming) == hipSuccess) {
-    x.s = st;
-    x.fork = f;
-    x.join = j;
-    return true;
-  }
-  if (f) (void)hipEventDestroy(f);
-  if (st) (void)hipStreamDestroy(st);
-  (void)hipGetLastError();  // clear the failed call's error
-  x.failed = true;
-  return false;
-}
-
 
 tri_status run_linear(const void* A, int lda, const void* B, int M, int N, int K, const Epi& epi,
                       float* part, hipStream_t s) {
@@ -555,17 +498,9 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
   const bool splitkv =
       decode || b->max_q_len == 1 || (int64_t)b->n_seqs * b->max_q_len != b->n_tokens;
   float* part_dec = (float*)((char*)part + flash_part_bytes(cfg, b));
-  hipStream_t sd = s;  // stream of the split-KV attention
-  SideStream* side = (flash && splitkv) ? side_stream(s) : nullptr;
-  std::unique_lock<std::mutex> side_lock;
-  if (side) {
-    side_lock = std::unique_lock<std::mutex>(side->mu);
-    if (side_ready(*side, s)) {
-      TRI_HIP(hipEventRecord(side->fork, s));
-      TRI_HIP(hipStreamWaitEvent(side->s, side->fork, 0));
-      sd = side->s;
-    }
-  }
+  Fork fork;
+  if (flash && splitkv) TRI_HIP(fork.begin(s));
+  hipStream_t sd = fork.stream ? fork.stream : s;  // stream of the split-KV attention
   if (splitkv) {
     {
       StageTimer t_(ST_ATTN_DECODE, sd, timed);
@@ -578,11 +513,7 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
     StageTimer t_(ST_ATTN_PREFILL, s, timed);
     TRI_HIP(launch_attn_prefill(q, cache->k, cache->v, attn, bd, kv, Hq, Hkv, D, 0, part, s));
   }
-  if (sd != s) {
-    TRI_HIP(hipEventRecord(side->join, sd));
-    TRI_HIP(hipStreamWaitEvent(s, side->join, 0));
-  }
-  if (side_lock.owns_lock()) side_lock.unlock();
+  TRI_HIP(fork.end());
   e = Epi{};
   e.kind = EPI_RESID;
   e.out = x1;

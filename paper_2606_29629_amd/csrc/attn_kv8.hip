@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "attn_kv8.hpp"
+#include "side.hpp"
 
 namespace tri {
 
@@ -293,66 +294,75 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, 
   if (lse && lg == 0) lse[at] = m_run + log2f(l_tot);
 }
 
-// Merge of the key-range splits, D / 4 threads per packed row, folded in split order.
+// Merge of the key-range splits: a workgroup per token and KV head, D / 4 threads per
+// query head, folded in split order.
 template <int D>
 __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
                                                             const float* __restrict__ part,
                                                             bf16* __restrict__ O,
                                                             float* __restrict__ lse, int nsplit) {
   constexpr int TPR = D / 4;
-  const int s = blockIdx.z, h = blockIdx.y, G = Hq / Hkv;
+  const int t = blockIdx.x, h = blockIdx.y, G = Hq / Hkv, lane = threadIdx.x & 63;
+  // the token's sequence: as many ends lie at or before it
+  int s = 0;
+  for (int j0 = 0; j0 < b.n_seqs; j0 += 64) {
+    const int end = b.cu_q[min(j0 + lane, b.n_seqs - 1) + 1];
+    s += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j0 + lane < b.n_seqs && end <= t));
+  }
   int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2) return;
-  const int row = blockIdx.x * (256 / TPR) + (int)threadIdx.x / TPR, rows = n * G;
-  if (row >= rows) return;
-  const int last = min(rows, (row / kRows8 + 1) * kRows8) - 1;  // of the flash kernel's tile
-  const int nkt = cdiv(ctx + last / G + 1, kKeys8), ns = cdiv(nkt, cdiv(nkt, nsplit));
-  const int64_t at = (int64_t)h * b.n_tokens * G + (int64_t)q0 * G + row;
+  if (s >= b.n_seqs || !kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2 || t < q0 || t >= q0 + n) return;
   const int64_t plane = (int64_t)b.n_tokens * Hq * (D + 4);
-  const float* pp = part + at * (D + 4);
   const int d = 4 * ((int)threadIdx.x % TPR);
-  f32x2 ml[kMaxSplitF8];
-  f32x4 a[kMaxSplitF8];
+  for (int g = (int)threadIdx.x / TPR; g < G; g += 256 / TPR) {
+    const int row = (t - q0) * G + g;
+    const int last = min(n * G, (row / kRows8 + 1) * kRows8) - 1;  // of the flash kernel's tile
+    const int nkt = cdiv(ctx + last / G + 1, kKeys8), ns = cdiv(nkt, cdiv(nkt, nsplit));
+    const int64_t at = (int64_t)h * b.n_tokens * G + (int64_t)q0 * G + row;
+    const float* pp = part + at * (D + 4);
+    f32x2 ml[kMaxSplitF8];
+    f32x4 a[kMaxSplitF8];
 #pragma unroll
-  for (int j = 0; j < kMaxSplitF8; ++j) {  // (splits past the last are loaded again and dropped)
-    const float* pj = pp + min(j, ns - 1) * plane;
-    ml[j] = *(const f32x2*)(pj + D);
-    a[j] = *(const f32x4*)(pj + d);
+    for (int j = 0; j < kMaxSplitF8; ++j) {  // (splits past the last are loaded again and dropped)
+      const float* pj = pp + min(j, ns - 1) * plane;
+      ml[j] = *(const f32x2*)(pj + D);
+      a[j] = *(const f32x4*)(pj + d);
+    }
+    float M = -INFINITY, L = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < kMaxSplitF8; ++j) {
+      if (j >= ns || (ml[j][0] == -INFINITY && ml[j][1] == 0.f)) continue;  // no key of it visible
+      const float Mn = fmaxf(M, ml[j][0]);
+      const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[j][0] - Mn);
+      L = L * x + ml[j][1] * w;
+      o = o * x + a[j] * w;
+      M = Mn;
+    }
+    bf16x4 o4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o4[e] = f2bf(o[e] / L);
+    *(bf16x4*)(O + ((int64_t)t * Hq + h * G + g) * D + d) = o4;
+    if (lse && d == 0) lse[at] = M + log2f(L);
   }
-  float M = -INFINITY, L = 0.f;
-  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < kMaxSplitF8; ++j) {
-    if (j >= ns || (ml[j][0] == -INFINITY && ml[j][1] == 0.f)) continue;  // no key of it visible
-    const float Mn = fmaxf(M, ml[j][0]);
-    const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[j][0] - Mn);
-    L = L * x + ml[j][1] * w;
-    o = o * x + a[j] * w;
-    M = Mn;
-  }
-  const int tok = row / G, hq = h * G + row - tok * G;
-  bf16x4 o4;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) o4[e] = f2bf(o[e] / L);
-  *(bf16x4*)(O + ((int64_t)(q0 + tok) * Hq + hq) * D + d) = o4;
-  if (lse && d == 0) lse[at] = M + log2f(L);
 }
 
 // mass[key] += sum over the packed rows of 2^(score - lse): the scores once more, keys and
-// rows the other way round.  One workgroup = 128 cache rows of a KV head, a wave 32 of
-// them with their codes in registers as bf16 (exact too, and q needs no conversion); rows
-// come 64 at a time through LDS by direct loads.  Every sum has one owner and one order.
+// rows the other way round.  One workgroup = 128 cache rows of a KV head, each of four wave
+// pairs 32 of them with their codes in registers as bf16 (exact too, and q needs no
+// conversion); query rows come 64 at a time through LDS by direct loads, 32 to each wave of
+// a pair, so that a SIMD's two waves cover each other's waits.  Every sum has one order.
 constexpr int kMassKeys = 128, kMassQ = 64;
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(256, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
+__global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
                                                                const bf16* __restrict__ Q, int64_t qs,
                                                                const float* __restrict__ lse,
                                                                float scale_log2e) {
   constexpr int DS = D / 16, DC = D / 8;
   constexpr int RPB = 64 / DC;             // rows of a 1 KB load
-  constexpr int NL = kMassQ / RPB / 4;     // such loads of a wave and tile
+  constexpr int NL = kMassQ / RPB / 8;     // such loads of a wave and tile
   __shared__ __align__(16) bf16 sq0[kMassQ * D], sq1[kMassQ * D];
+  __shared__ float upper[4][32];
   const int s = blockIdx.z, h = blockIdx.y, key0 = blockIdx.x * kMassKeys;
   int q0, n, ctx, sl;
   if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2 || key0 >= ctx + n) return;
@@ -361,7 +371,7 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lg = lane >> 5;
   // codes of this wave's 32 keys: lane key lr, values 16 t + 8 lg ...
-  const int wkey = key0 + 32 * wave;
+  const int half = wave >> 2, wkey = key0 + 32 * (wave & 3);
   int prow = 0;
   const int panel = wkey < ctx + n ? kv_panel(c.kv, sl, wkey, prow) : -1;
   const int live = panel < 0 ? 0 : min(32, ctx + n - wkey);
@@ -392,7 +402,7 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
         (void*)(Q + (int64_t)(q0 + tok0) * qs + (int64_t)h * G * D), (short)0, 0x7fffffff, 0x00020000);
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const int blk = wave + 4 * j, r = blk * RPB + lane / DC;
+      const int blk = wave + 8 * j, r = blk * RPB + lane / DC;
       const int row = min(rt * kMassQ + r, rows - 1), tok = row / G;
       const uint32_t off = (uint32_t)((tok - tok0) * (int)qs + (row - tok * G) * D + kv_chunk<D>(lane % DC, r) * 8) * 2;
       buffer_load_lds16(rq, dst + blk * 512, off, 0);
@@ -402,42 +412,59 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
   const float* lp = lse + (int64_t)h * b.n_tokens * G + (int64_t)q0 * G;
+  auto lse_of = [&](int rt) {
+    const int row = rt * kMassQ + 32 * half + lr;
+    return row < rows ? lp[row] : INFINITY;
+  };
+  float off_next = lse_of(rt_lo);
   gload(rt_lo, Int<0>{});
   auto step = [&](int rt, auto buf) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (rt + 1 < rt_hi) gload(rt + 1, Int<1 - decltype(buf)::value>{});
+    const float off = off_next;
+    if (rt + 1 < rt_hi) {
+      off_next = lse_of(rt + 1);  // (before the rows: loads come back in order)
+      gload(rt + 1, Int<1 - decltype(buf)::value>{});
+    }
     const bf16* qb = decltype(buf)::value ? sq1 : sq0;
+    const int r = 32 * half + lr, row = rt * kMassQ + r;
+    const int qpos = ctx + min(row, rows - 1) / G;
+    f32x16 sc = f32x16{0.f};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = 32 * u + lr, row = rt * kMassQ + r;
-      const bool there = row < rows;
-      const float off = there ? lp[row] : INFINITY;
-      const int qpos = ctx + min(row, rows - 1) / G;
-      f32x16 sc = f32x16{0.f};
-#pragma unroll
-      for (int t = 0; t < DS; ++t)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            kreg[t], *(const bf16x8*)&qb[r * D + kv_chunk<D>(2 * t + lg, r) * 8], sc, 0, 0, 0);
-      const bool edge = wkey + 31 > ctx + rt * kMassQ / G;  // some row may not see some key
+    for (int t = 0; t < DS; ++t)
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          kreg[t], *(const bf16x8*)&qb[r * D + kv_chunk<D>(2 * t + lg, r) * 8], sc, 0, 0, 0);
+    // (rows past the end: 2^-inf)
+    if (wkey + 31 > ctx + rt * kMassQ / G) {  // some row may not see some key
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float w = __builtin_amdgcn_exp2f(fmaf(sc[e], kf, -off));
-        const int key = wkey + (e & 3) + 8 * (e >> 2) + 4 * lg;
-        acc[e] += there && (!edge || key <= qpos) ? w : 0.f;
+        acc[e] += wkey + (e & 3) + 8 * (e >> 2) + 4 * lg <= qpos ? w : 0.f;
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] += __builtin_amdgcn_exp2f(fmaf(sc[e], kf, -off));
     }
   };
   for (int rt = rt_lo; rt < rt_hi; rt += 2) {
     step(rt, Int<0>{});
     if (rt + 1 < rt_hi) step(rt + 1, Int<1>{});
   }
+  // the pair's halves: the upper one's sums through LDS
   float* mp = c.mass + kv8_row_at(c, Hkv, max(panel, 0), h, prow);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const float sum = group_sum(acc[e], 32);
-    const int k = (e & 3) + 8 * (e >> 2) + 4 * lg;
-    if (lr == 0 && k < live) mp[k] += sum;
+  for (int e = 0; e < 16; ++e) acc[e] = group_sum(acc[e], 32);
+  if (half == 1 && lr == 0) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) upper[wave & 3][(e & 3) + 8 * (e >> 2) + 4 * lg] = acc[e];
+  }
+  __syncthreads();
+  if (half == 0 && lr == 0) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int k = (e & 3) + 8 * (e >> 2) + 4 * lg;
+      if (k < live) mp[k] += acc[e] + upper[wave][k];
+    }
   }
 }
 
@@ -490,12 +517,12 @@ static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv
   else e = c.kv.table ? go(attn_kv8_kernel<D, FP8, true, false>) : go(attn_kv8_kernel<D, FP8, false, false>);
   if (e != hipSuccess) return e;
   if (sp > 1) {
-    attn_kv8_fold_kernel<D><<<dim3(cdiv(b.max_q_len * G, 1024 / D), Hkv, b.n_seqs), 256, 0, s>>>(
+    attn_kv8_fold_kernel<D><<<dim3(b.n_tokens, Hkv), 256, 0, s>>>(
         b, c, Hq, Hkv, part, (bf16*)out, lse, sp);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (c.mass) {
-    attn_kv8_mass_kernel<D, FP8><<<dim3(cdiv(b.max_ctx_len + b.max_q_len, kMassKeys), Hkv, b.n_seqs), 256, 0, s>>>(
+    attn_kv8_mass_kernel<D, FP8><<<dim3(cdiv(b.max_ctx_len + b.max_q_len, kMassKeys), Hkv, b.n_seqs), 512, 0, s>>>(
         b, c, Hq, Hkv, (const bf16*)q, qs, lse, scale_log2e);
     e = hipGetLastError();
   }
@@ -506,17 +533,29 @@ hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q
                            int n_kv_heads, int head_dim, const void* q, int64_t q_stride, void* out,
                            void* ws, hipStream_t s) {
   if (b.n_seqs == 0 || b.n_tokens == 0) return hipSuccess;
-  if (b.max_q_len == 1 || (int64_t)b.n_seqs * b.max_q_len != b.n_tokens) {
-    float* own = (float*)((char*)ws + lse_bytes(b, c, n_q_heads) + part8_bytes(b, n_q_heads, n_kv_heads, head_dim));
-    const hipError_t e = launch_attn_kv8_decode(b, c, fp8, n_q_heads, n_kv_heads, head_dim, q, q_stride, out, own, s);
-    if (e != hipSuccess || b.max_q_len == 1) return e;
-  }
   char* w = (char*)ws;
-  if (head_dim == 128)
-    return fp8 ? run_flash8<128, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
-               : run_flash8<128, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
-  return fp8 ? run_flash8<64, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
-             : run_flash8<64, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
+  float* own = (float*)(w + lse_bytes(b, c, n_q_heads) + part8_bytes(b, n_q_heads, n_kv_heads, head_dim));
+  auto singles = [&](hipStream_t st) {
+    return launch_attn_kv8_decode(b, c, fp8, n_q_heads, n_kv_heads, head_dim, q, q_stride, out, own, st);
+  };
+  if (b.max_q_len == 1) return singles(s);
+  // Single tokens beside chunks: on the side stream (memory-bound beside compute-bound;
+  // other output rows, other weights' rows, another part of the workspace).
+  Fork fork;
+  hipError_t e = hipSuccess;
+  if ((int64_t)b.n_seqs * b.max_q_len != b.n_tokens) {
+    if ((e = fork.begin(s)) == hipSuccess) e = singles(fork.stream);
+  }
+  if (e == hipSuccess) {
+    if (head_dim == 128)
+      e = fp8 ? run_flash8<128, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
+              : run_flash8<128, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
+    else
+      e = fp8 ? run_flash8<64, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
+              : run_flash8<64, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
+  }
+  const hipError_t j = fork.end();
+  return e != hipSuccess ? e : j;
 }
 
 }  // namespace tri

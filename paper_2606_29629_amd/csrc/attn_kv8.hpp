@@ -7,11 +7,6 @@ namespace tri {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 
-template <int N>
-struct Int {
-  static constexpr int value = N;
-};
-
 // Splits of a batch's rows: how many, rows of each (a multiple of the tile), and a bound
 // on how many that never falls as the rows grow.
 struct Kv8Splits {

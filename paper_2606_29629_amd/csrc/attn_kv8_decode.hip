@@ -286,88 +286,104 @@ __global__ __launch_bounds__(64, 2) void attn_kv8_decode_kernel(
   if (g == 0) *(f32x2*)(pp + D) = f32x2{m_run, l_run};
 }
 
-// Merge of a single token's splits, and the sums of its attention weights.  Workgroups
-// x < Hq: query head x; M = max m_j, L = sum l_j 2^(m_j - M), out = sum O_j 2^(m_j - M) / L,
-// eight threads' worth of splits side by side.  The others: kMassRows rows of a KV head;
-// mass[row] += sum over the heads of 2^(score - M - log2 L).
+// The sums of a single token's attention weights, and the merge of its splits.
+// Workgroups x < mass_wgs (the longer ones, first): kMassRows rows of a KV head, four
+// neighbouring rows a thread; mass[row] += sum over the heads of 2^(score - M - log2 L).
+// The others: query head x; M = max m_j, L = sum l_j 2^(m_j - M), out = sum O_j 2^(m_j -
+// M) / L, TS threads' worth of splits side by side.
 constexpr int kMassRows = 1024;
 
 template <int D>
 __global__ __launch_bounds__(256) void attn_kv8_merge_kernel(
     BatchDev b, Kv8Dev c, int Hq, int Hkv, const float* __restrict__ part, bf16* __restrict__ O,
-    const float* __restrict__ scores, int score_ld, int nsplit, int split_rows) {
+    const float* __restrict__ scores, int score_ld, int nsplit, int split_rows, int mass_wgs) {
   constexpr int TD = D / 4, TS = 256 / TD;  // threads over d, and over splits
   __shared__ float red[TS][D];
-  __shared__ float lse[32];
+  __shared__ float lse[32], ms[TS], ls[TS];
   const int s = blockIdx.y, tid = threadIdx.x;
   int t, n, ctx, sl;
   if (!kv8_seq(b, c, s, t, n, ctx, sl) || n != 1) return;
   const int rows_seen = min(ctx, b.max_ctx_len) + 1;
   const int ns = min(cdiv(rows_seen, split_rows), nsplit);
   const int lane = tid & 63, wave = tid >> 6;
-  if ((int)blockIdx.x < Hq) {
-    const int qh = blockIdx.x;
-    const float* pp = part + ((int64_t)s * Hq + qh) * nsplit * (D + 4);
-    const int d = 4 * (tid % TD), j0 = tid / TD;
-    float M = -INFINITY, L = 0.f;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int j = j0; j < ns; j += TS) {
-      const float* q = pp + (int64_t)j * (D + 4);
-      const f32x2 ml = *(const f32x2*)(q + D);
-      const f32x4 a = *(const f32x4*)(q + d);
-      const float Mn = fmaxf(M, ml[0]);
-      const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[0] - Mn);
-      L = L * x + ml[1] * w;
-      o = o * x + a * w;
-      M = Mn;
-    }
-    // the TS threads of a d: through LDS in order, with the common maximum
-    __shared__ float ms[TS], ls[TS];
-    if (tid % TD == 0) ms[j0] = M;
-    __syncthreads();
-    float top = ms[0];
-#pragma unroll
-    for (int j = 1; j < TS; ++j) top = fmaxf(top, ms[j]);
-    const float w = j0 < ns ? exp2f(M - top) : 0.f;
-    if (tid % TD == 0) ls[j0] = j0 < ns ? L * w : 0.f;
-    *(f32x4*)&red[j0][d] = j0 < ns ? o * w : f32x4{0.f, 0.f, 0.f, 0.f};
-    __syncthreads();
-    if (tid < D) {
-      float sum = 0.f, l = 0.f;
-#pragma unroll
-      for (int j = 0; j < TS; ++j) {
-        sum += red[j][tid];
-        l += ls[j];
+  if ((int)blockIdx.x < mass_wgs) {
+    const int grp = Hq / Hkv, chunks = mass_wgs / Hkv;
+    const int h = (int)blockIdx.x / chunks, row0 = ((int)blockIdx.x % chunks) * kMassRows;
+    if (row0 >= rows_seen) return;
+    for (int q = wave; q < grp; q += 4) {
+      const float* pp = part + ((int64_t)s * Hq + h * grp + q) * nsplit * (D + 4) + D;
+      float M = -INFINITY, L = 0.f;
+      for (int j = lane; j < ns; j += 64) {
+        const f32x2 ml = *(const f32x2*)(pp + (int64_t)j * (D + 4));
+        const float Mn = fmaxf(M, ml[0]);
+        L = (M == -INFINITY ? 0.f : L * exp2f(M - Mn)) + ml[1] * exp2f(ml[0] - Mn);
+        M = Mn;
       }
-      O[((int64_t)t * Hq + qh) * D + tid] = f2bf(sum / l);
+      const float top = wave_max(M);
+      L = wave_sum(lane < ns ? L * exp2f(M - top) : 0.f);
+      if (lane == 0) lse[q] = top + log2f(L);
     }
+    __syncthreads();
+    const int row = row0 + 4 * tid;
+    int prow = 0;
+    const int panel = row < rows_seen ? kv_panel(c.kv, sl, row, prow) : -1;
+    if (panel < 0) return;
+    const float* sp = scores + ((int64_t)s * Hq + h * grp) * score_ld + row;
+    float* mp = c.mass + kv8_row_at(c, Hkv, panel, h, prow);
+    float before[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) before[e] = row + e < rows_seen ? mp[e] : 0.f;
+    f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int q0 = 0; q0 < grp; q0 += 4) {
+      f32x4 x[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = *(const f32x4*)(sp + (int64_t)min(q0 + q, grp - 1) * score_ld);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q0 + q >= grp) break;
+        const float off = lse[q0 + q];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(x[q][e] - off);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (row + e < rows_seen) mp[e] = before[e] + sum[e];
     return;
   }
-  const int grp = Hq / Hkv, chunks = ((int)gridDim.x - Hq) / Hkv;
-  const int h = ((int)blockIdx.x - Hq) / chunks, row0 = (((int)blockIdx.x - Hq) % chunks) * kMassRows;
-  if (row0 >= rows_seen) return;
-  for (int q = wave; q < grp; q += 4) {
-    const float* pp = part + ((int64_t)s * Hq + h * grp + q) * nsplit * (D + 4) + D;
-    float M = -INFINITY, L = 0.f;
-    for (int j = lane; j < ns; j += 64) {
-      const f32x2 ml = *(const f32x2*)(pp + (int64_t)j * (D + 4));
-      const float Mn = fmaxf(M, ml[0]);
-      L = (M == -INFINITY ? 0.f : L * exp2f(M - Mn)) + ml[1] * exp2f(ml[0] - Mn);
-      M = Mn;
-    }
-    const float top = wave_max(M);
-    L = wave_sum(lane < ns ? L * exp2f(M - top) : 0.f);
-    if (lane == 0) lse[q] = top + log2f(L);
+  const int qh = (int)blockIdx.x - mass_wgs;
+  const float* pp = part + ((int64_t)s * Hq + qh) * nsplit * (D + 4);
+  const int d = 4 * (tid % TD), j0 = tid / TD;
+  float M = -INFINITY, L = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int j = j0; j < ns; j += TS) {
+    const float* q = pp + (int64_t)j * (D + 4);
+    const f32x2 ml = *(const f32x2*)(q + D);
+    const f32x4 a = *(const f32x4*)(q + d);
+    const float Mn = fmaxf(M, ml[0]);
+    const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[0] - Mn);
+    L = L * x + ml[1] * w;
+    o = o * x + a * w;
+    M = Mn;
   }
+  // the TS threads of a d: through LDS in order, with the common maximum
+  if (tid % TD == 0) ms[j0] = M;
   __syncthreads();
-  for (int row = row0 + tid; row < min(rows_seen, row0 + kMassRows); row += 256) {
-    int prow;
-    const int panel = kv_panel(c.kv, sl, row, prow);
-    if (panel < 0) continue;
-    float sum = 0.f;
-    for (int q = 0; q < grp; ++q)
-      sum += __builtin_amdgcn_exp2f(scores[((int64_t)s * Hq + h * grp + q) * score_ld + row] - lse[q]);
-    c.mass[kv8_row_at(c, Hkv, panel, h, prow)] += sum;
+  float top = ms[0];
+#pragma unroll
+  for (int j = 1; j < TS; ++j) top = fmaxf(top, ms[j]);
+  const float w = j0 < ns ? exp2f(M - top) : 0.f;
+  if (tid % TD == 0) ls[j0] = j0 < ns ? L * w : 0.f;
+  *(f32x4*)&red[j0][d] = j0 < ns ? o * w : f32x4{0.f, 0.f, 0.f, 0.f};
+  __syncthreads();
+  if (tid < D) {
+    float sum = 0.f, l = 0.f;
+#pragma unroll
+    for (int j = 0; j < TS; ++j) {
+      sum += red[j][tid];
+      l += ls[j];
+    }
+    O[((int64_t)t * Hq + qh) * D + tid] = f2bf(sum / l);
   }
 }
 
@@ -398,9 +414,9 @@ static hipError_t run_decode8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hk
   hipError_t e = c.kv.table ? go(attn_kv8_decode_kernel<D, FP8, true>)
                             : go(attn_kv8_decode_kernel<D, FP8, false>);
   if (e != hipSuccess) return e;
-  const int more = c.mass ? Hkv * cdiv(max_kv, kMassRows) : 0;
-  attn_kv8_merge_kernel<D><<<dim3(Hq + more, b.n_seqs), 256, 0, s>>>(
-      b, c, Hq, Hkv, part, (bf16*)out, scores, ld, sp.n, sp.rows);
+  const int mass_wgs = c.mass ? Hkv * cdiv(max_kv, kMassRows) : 0;
+  attn_kv8_merge_kernel<D><<<dim3(mass_wgs + Hq, b.n_seqs), 256, 0, s>>>(
+      b, c, Hq, Hkv, part, (bf16*)out, scores, ld, sp.n, sp.rows, mass_wgs);
   return hipGetLastError();
 }
 

@@ -179,13 +179,17 @@ constexpr int select_hist_at(int pass) { return pass * 2048; }
 
 // The bin in which the counts from the top reach `need`, and the count above it.  W waves;
 // `red` holds W words, `found` two; every thread gets the answer.
-template <int W>
-__device__ __forceinline__ void select_bin(const uint32_t* hist, int bins, int need, uint32_t* red,
+template <int W, int BINS>
+__device__ __forceinline__ void select_bin(const uint32_t* hist, int need, uint32_t* red,
                                            uint32_t* found, int& bin, int& above) {
+  constexpr int PER = BINS / (64 * W);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = bins / (64 * W);
-  uint32_t mine = 0;
-  for (int i = 0; i < per; ++i) mine += hist[bins - 1 - (tid * per + i)];
+  uint32_t cnt[PER], mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    cnt[i] = hist[BINS - 1 - (tid * PER + i)];
+    mine += cnt[i];
+  }
   uint32_t upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -197,14 +201,13 @@ __device__ __forceinline__ void select_bin(const uint32_t* hist, int bins, int n
   uint32_t over = upto - mine;
 #pragma unroll
   for (int w = 0; w < W; ++w) over += w < wave ? red[w] : 0u;
-  for (int i = 0; i < per; ++i) {
-    const int at = bins - 1 - (tid * per + i);
-    const uint32_t cnt = hist[at];
-    if (over < (uint32_t)need && over + cnt >= (uint32_t)need) {
-      found[0] = (uint32_t)at;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (over < (uint32_t)need && over + cnt[i] >= (uint32_t)need) {
+      found[0] = (uint32_t)(BINS - 1 - (tid * PER + i));
       found[1] = over;
     }
-    over += cnt;
+    over += cnt[i];
   }
   __syncthreads();
   bin = (int)found[0];
@@ -277,21 +280,23 @@ __global__ __launch_bounds__(kSelThreads) void kv8_select_kernel(BatchDev b, Kv8
   }
   uint32_t T = 0;
   int need = budget;
-#pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = select_shift(pass), bins = select_bins(pass);
-    const uint32_t mask = pass == 0 ? 0u : ~0u << select_shift(pass - 1);
-    for (int i = tid; i < bins; i += kSelThreads) hist[i] = 0;
+  auto digit = [&](auto pass_) {
+    constexpr int PASS = decltype(pass_)::value, SHIFT = select_shift(PASS), BINS = select_bins(PASS);
+    constexpr uint32_t mask = PASS == 0 ? 0u : ~0u << (PASS == 1 ? 21 : 10);
+    for (int i = tid; i < BINS; i += kSelThreads) hist[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < K; ++i)
-      if (r0 + i < n && (key[i] & mask) == T) atomicAdd(&hist[(key[i] >> shift) & (bins - 1)], 1u);
+      if (r0 + i < n && (key[i] & mask) == T) atomicAdd(&hist[(key[i] >> SHIFT) & (BINS - 1)], 1u);
     __syncthreads();
     int bin, above;
-    select_bin<W>(hist, bins, need, red, found, bin, above);
-    T |= (uint32_t)bin << shift;
+    select_bin<W, BINS>(hist, need, red, found, bin, above);
+    T |= (uint32_t)bin << SHIFT;
     need -= above;
-  }
+  };
+  digit(Int<0>{});
+  digit(Int<1>{});
+  digit(Int<2>{});
   // Kept before a row: the greater keys and the first `need` equal ones.
   int gt = 0, eq = 0;
 #pragma unroll
@@ -301,13 +306,13 @@ __global__ __launch_bounds__(kSelThreads) void kv8_select_kernel(BatchDev b, Kv8
   }
   int ngt, neq, all_gt, all_eq;
   block_prefix2<W>(gt, eq, ngt, neq, all_gt, all_eq, sums);
-  int place[K];  // kept rows before each row
-  bool keep[K];
+  int place[K];       // kept rows before each row
+  uint32_t keep = 0;  // bit i: row i stays
 #pragma unroll
   for (int i = 0; i < K; ++i) {
-    const bool there = r0 + i < n, more = there && key[i] > T, same = there && key[i] == T;
+    const int more = r0 + i < n && key[i] > T, same = r0 + i < n && key[i] == T;
     place[i] = ngt + min(neq, need);
-    keep[i] = more || (same && neq < need);
+    keep |= (uint32_t)(more | (same & (int)(neq < need))) << i;
     if (r0 + i == budget) kept_low_at = place[i];
     ngt += more;
     neq += same;
@@ -316,12 +321,12 @@ __global__ __launch_bounds__(kSelThreads) void kv8_select_kernel(BatchDev b, Kv8
   const int kept_low = kept_low_at;
 #pragma unroll
   for (int i = 0; i < K; ++i)
-    if (keep[i] && r0 + i >= budget) list[place[i] - kept_low] = r0 + i;
+    if ((keep >> i & 1) && r0 + i >= budget) list[place[i] - kept_low] = r0 + i;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < K; ++i) {
     const int r = r0 + i;
-    if (r < budget) out[r] = keep[i] ? r : list[r - place[i]];
+    if (r < budget) out[r] = (keep >> i & 1) ? r : list[r - place[i]];
   }
 }
 
@@ -331,6 +336,7 @@ __global__ __launch_bounds__(kSelThreads) void kv8_select_kernel(BatchDev b, Kv8
 struct SelectWs {
   uint32_t *key, *hist, *newest;
   int32_t *count, *list;
+  uint2* state;  // T's digits so far, equal keys still needed (after pass 0 at 0, ...)
   int chunks, list_rows;
   __device__ uint32_t* keys_of(int64_t p) const { return key + p * chunks * kSelChunk; }
   __device__ uint32_t* hist_of(int64_t p, int pass) const { return hist + p * kSelHist + select_hist_at(pass); }
@@ -360,21 +366,19 @@ __global__ __launch_bounds__(256) void select_newest_kernel(BatchDev b, Kv8Dev c
   if (threadIdx.x == 0) w.newest[pair * w.chunks + blockIdx.x] = top;
 }
 
-// T's digits and the equal keys still needed after the first `passes` histograms.
-template <int PASSES>
-__device__ __forceinline__ uint32_t select_digits(const SelectWs& w, int64_t pair, int budget,
-                                                  uint32_t* red, uint32_t* found, int& need) {
-  uint32_t T = 0;
-  need = budget;
-#pragma unroll
-  for (int pass = 0; pass < PASSES; ++pass) {
-    int bin, above;
-    __syncthreads();
-    select_bin<4>(w.hist_of(pair, pass), select_bins(pass), need, red, found, bin, above);
-    T |= (uint32_t)bin << select_shift(pass);
-    need -= above;
-  }
-  return T;
+// T's digits and the equal keys still needed after histogram PASS: one scan on what the
+// launch before had found, kept for the next one by the first chunk.
+template <int PASS>
+__device__ __forceinline__ uint32_t select_digit(const SelectWs& w, int64_t pair, int budget,
+                                                 uint32_t* red, uint32_t* found, int& need) {
+  uint2 st = PASS == 0 ? make_uint2(0u, (uint32_t)budget) : w.state[2 * pair + PASS - 1];
+  int bin, above;
+  select_bin<4, select_bins(PASS)>(w.hist_of(pair, PASS), (int)st.y, red, found, bin, above);
+  st.x |= (uint32_t)bin << select_shift(PASS);
+  st.y -= (uint32_t)above;
+  if (PASS < 2 && blockIdx.x == 0 && threadIdx.x == 0) w.state[2 * pair + PASS] = st;
+  need = (int)st.y;
+  return st.x;
 }
 
 template <int PASS>
@@ -408,7 +412,7 @@ __global__ __launch_bounds__(256) void select_hist_kernel(BatchDev b, Kv8Dev c, 
 #pragma unroll
     for (int i = 0; i < kSelK; ++i) key[i] = i < 4 ? x[i] : y[i - 4];
     int need;
-    T = select_digits<PASS>(w, pair, budget, red, found, need);
+    T = select_digit<PASS - 1>(w, pair, budget, red, found, need);
     mask = ~0u << select_shift(PASS - 1);
   }
   __syncthreads();
@@ -445,7 +449,7 @@ __global__ __launch_bounds__(256) void select_place_kernel(BatchDev b, Kv8Dev c,
   const u32x4* kp = (const u32x4*)(w.keys_of(pair) + r0);
   const u32x4 x = kp[0], y = kp[1];
   int need;
-  const uint32_t T = select_digits<3>(w, pair, budget, red, found, need);
+  const uint32_t T = select_digit<2>(w, pair, budget, red, found, need);
   uint32_t key[kSelK];
   int gt = 0, eq = 0, gt_low = 0, eq_low = 0;  // (low: rows below budget)
 #pragma unroll
@@ -513,7 +517,7 @@ size_t kv8_select_workspace_bytes(const BatchDev& b, int n_kv_heads, int budget)
   if (most <= kSelOneRows || most <= budget) return 0;
   const size_t pairs = (size_t)b.n_seqs * n_kv_heads, chunks = cdiv(most, kSelChunk);
   const size_t list = std::min(budget, most - budget);
-  return 4 * pairs * (chunks * kSelChunk + kSelHist + chunks * 5 + (list + 3) / 4 * 4) + 64;
+  return 4 * pairs * (chunks * kSelChunk + kSelHist + chunks * 5 + 4 + list);
 }
 
 hipError_t launch_kv8_select(const BatchDev& b, const Kv8Dev& c, int n_kv_heads, int budget,
@@ -537,7 +541,8 @@ hipError_t launch_kv8_select(const BatchDev& b, const Kv8Dev& c, int n_kv_heads,
   w.chunks = cdiv(most, kSelChunk);
   w.list_rows = std::min(budget, most - budget);
   w.key = (uint32_t*)ws;
-  w.count = (int32_t*)(w.key + pairs * w.chunks * kSelChunk);
+  w.state = (uint2*)(w.key + pairs * w.chunks * kSelChunk);
+  w.count = (int32_t*)(w.state + 2 * pairs);
   w.hist = (uint32_t*)(w.count + pairs * w.chunks * 4);
   w.newest = w.hist + pairs * kSelHist;
   w.list = (int32_t*)(w.newest + pairs * w.chunks);
@@ -552,80 +557,132 @@ hipError_t launch_kv8_select(const BatchDev& b, const Kv8Dev& c, int n_kv_heads,
   return hipGetLastError();
 }
 
-// Move.  One workgroup per (scale block below budget, head, sequence).  Rows come from
-// at or past budget and go below it, so no workgroup reads what another writes.  Most
-// blocks of a lightly trimmed cache change nothing and end at their plan entries.
-template <int D, bool FP8>
-__global__ __launch_bounds__(256) void kv8_move_kernel(BatchDev b, Kv8Dev c, int Hkv,
+// Move.  One wave per (32 rows below budget, head, sequence), four to a workgroup.  Rows
+// come from at or past budget and go below it, so no wave reads rows that another writes;
+// the waves of one scale block (R = 32 WPB rows) each find its largest scale, and meet once
+// before it is written.  A wave's rows are few and its loads depend on each other (plan,
+// page, scales, codes), so the waves in flight bound it: sources stay in registers and all
+// pieces of codes are in flight at once.  Blocks that nothing moves into end at their plan
+// entries.  (64 sequences of 4352 rows to 4096, 4 heads of 128: %MOVE%.)
+template <int D, bool FP8, int WPB>
+__global__ __launch_bounds__(256) void kv8_move_kernel(BatchDev b, Kv8Dev c, int Hkv, int blocks,
                                                        const int32_t* __restrict__ plan, int budget) {
-  constexpr int CPR = D / 16, kMaxRows = 128;
-  __shared__ int64_t src_row[kMaxRows];  // row index of the source, -1: leave the row
-  __shared__ float src_scale[2][kMaxRows];
-  __shared__ uint32_t red[2][4];
-  const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+  constexpr int CPR = D / 16, R = 32 * WPB, RPL = WPB == 4 ? 2 : 1, ITEMS = 32 * CPR / 64;
+  const int s = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 63;
+  const int wave = (int)(threadIdx.x >> 6), sub = wave % WPB;
+  const int blk = blockIdx.x * (4 / WPB) + wave / WPB, r0 = blk * R;
   const int sl = b.slot[s];
   if (sl < 0 || sl >= c.kv.n_slots) return;
-  const int R = 1 << c.scale_shift, r0 = blockIdx.x << c.scale_shift;
-  int prow;
-  const int panel = kv_panel(c.kv, sl, r0, prow);
-  if (panel < 0) return;
-  int src = -1;
-  if (tid < R) {
-    src = plan[((int64_t)s * Hkv + h) * budget + r0 + tid];
-    if (src < 0 || src >= c.kv.max_seq) src = -1;
+  int prow = 0;
+  const int panel = blk < blocks ? kv_panel(c.kv, sl, r0, prow) : -1;
+  // Lane j: rows j and (R = 128) j + 64 of the block.
+  const int32_t* pl = plan + ((int64_t)s * Hkv + h) * budget + r0;
+  int src[RPL];
+  bool any = false;
+#pragma unroll
+  for (int j = 0; j < RPL; ++j) {
+    const int r = lane + 64 * j;
+    src[j] = panel >= 0 && r < R ? pl[r] : -1;
+    if (src[j] >= c.kv.max_seq) src[j] = -1;
+    any |= src[j] >= 0 && src[j] != r0 + r;
   }
-  if (!__syncthreads_or(src >= 0 && src != r0 + tid)) return;
-  const int64_t row0 = kv8_row_at(c, Hkv, panel, h, prow), at = kv8_scale_at(c, Hkv, panel, h, prow);
-  uint32_t ks = 0, vs = 0;
-  if (tid < R) {
-    int64_t from = -1;
-    if (src >= 0) {
-      int p;
-      const int sp = kv_panel(c.kv, sl, src, p);
-      if (sp >= 0) {
-        from = kv8_row_at(c, Hkv, sp, h, p);
-        const int64_t sa = kv8_scale_at(c, Hkv, sp, h, p);
-        src_scale[0][tid] = c.k_scale[sa];
-        src_scale[1][tid] = c.v_scale[sa];
-        ks = __float_as_uint(src_scale[0][tid]) & 0x7fffffffu;
-        vs = __float_as_uint(src_scale[1][tid]) & 0x7fffffffu;
+  const bool live = __builtin_amdgcn_ballot_w64(any) != 0;
+  const int64_t row0 = kv8_row_at(c, Hkv, max(panel, 0), h, prow);
+  const int64_t at = kv8_scale_at(c, Hkv, max(panel, 0), h, prow);
+  int64_t from[RPL];  // row index of the source, -1: leave the row
+  float now[2], f[2][RPL];  // the block's scales; factor of each row's codes, 1: as they are
+  if (live) {
+    float scale[2][RPL];
+    uint32_t top[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < RPL; ++j) {
+      from[j] = -1;
+      scale[0][j] = scale[1][j] = 0.f;
+      if (src[j] >= 0) {
+        int p;
+        const int sp = kv_panel(c.kv, sl, src[j], p);
+        if (sp >= 0) {
+          from[j] = kv8_row_at(c, Hkv, sp, h, p);
+          const int64_t sa = kv8_scale_at(c, Hkv, sp, h, p);
+          scale[0][j] = c.k_scale[sa];
+          scale[1][j] = c.v_scale[sa];
+        }
+      }
+      top[0] = max(top[0], __float_as_uint(scale[0][j]) & 0x7fffffffu);
+      top[1] = max(top[1], __float_as_uint(scale[1][j]) & 0x7fffffffu);
+    }
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      now[kv] = __uint_as_float(block_max<1>(top[kv], nullptr));
+      const float inv = kv8_inverse(now[kv]);
+#pragma unroll
+      for (int j = 0; j < RPL; ++j) f[kv][j] = scale[kv][j] == scale[kv][j] ? scale[kv][j] * inv : 0.f;
+    }
+    // the wave's own rows 32 sub ..
+    u32x4 x[2][ITEMS];
+    float fac[2][ITEMS];
+    uint32_t work = 0;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      const int i = 64 * j + lane, r = 32 * sub + i / CPR, d = (i % CPR) * 16, l = r & 63;
+      int64_t fr = __shfl(from[0], l, 64);
+      fac[0][j] = __shfl(f[0][0], l, 64);
+      fac[1][j] = __shfl(f[1][0], l, 64);
+      if constexpr (RPL == 2) {
+        const int64_t fr1 = __shfl(from[1], l, 64);
+        const float a = __shfl(f[0][1], l, 64), e = __shfl(f[1][1], l, 64);
+        fr = r >= 64 ? fr1 : fr;
+        fac[0][j] = r >= 64 ? a : fac[0][j];
+        fac[1][j] = r >= 64 ? e : fac[1][j];
+      }
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const bool go = fr >= 0 && !(fr == row0 + r && fac[kv][j] == 1.f);
+        work |= (uint32_t)go << (2 * j + kv);
+        if (go) x[kv][j] = ldg16((kv ? c.v : c.k) + fr * D + d);
       }
     }
-    src_row[tid] = from;
-  }
-  const float now[2] = {__uint_as_float(block_max<4>(ks, red[0])),
-                        __uint_as_float(block_max<4>(vs, red[1]))};
-  __syncthreads();
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    uint8_t* codes = kv ? c.v : c.k;
-    const float inv = kv8_inverse(now[kv]);
-    for (int i = tid; i < R * CPR; i += 256) {
-      const int r = i / CPR, d = (i % CPR) * 16;
-      const int64_t from = src_row[r], to = row0 + r;
-      const float sc = src_scale[kv][r];
-      if (from < 0 || (from == to && sc == now[kv])) continue;
-      stg16(codes + to * D + d,
-            kv8_rescale16<FP8>(ldg16(codes + from * D + d), sc == sc ? sc * inv : 0.f));
+    for (int j = 0; j < ITEMS; ++j) {
+      const int i = 64 * j + lane, r = 32 * sub + i / CPR, d = (i % CPR) * 16;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv)
+        if (work >> (2 * j + kv) & 1) {
+          if (fac[kv][j] != 1.f) x[kv][j] = kv8_rescale16<FP8>(x[kv][j], fac[kv][j]);
+          stg16((kv ? c.v : c.k) + (row0 + r) * D + d, x[kv][j]);
+        }
     }
-    if (tid == 0) (kv ? c.v_scale : c.k_scale)[at] = now[kv];
+#pragma unroll
+    for (int j = 0; j < RPL; ++j) {
+      const int r = lane + 64 * j;
+      if (sub == 0 && from[j] >= 0 && from[j] != row0 + r) {
+        if (c.mass) c.mass[row0 + r] = c.mass[from[j]];
+        if (c.stamp) c.stamp[row0 + r] = c.stamp[from[j]];
+      }
+    }
   }
-  if (tid < R && src_row[tid] >= 0 && src_row[tid] != row0 + tid) {
-    if (c.mass) c.mass[row0 + tid] = c.mass[src_row[tid]];
-    if (c.stamp) c.stamp[row0 + tid] = c.stamp[src_row[tid]];
+  if constexpr (WPB > 1) __syncthreads();  // every wave of the block has read its scales
+  if (live && sub == 0 && lane == 0) {
+    c.k_scale[at] = now[0];
+    c.v_scale[at] = now[1];
   }
 }
 
 hipError_t launch_kv8_move(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_kv_heads,
                            int head_dim, const int32_t* plan, int budget, hipStream_t s) {
   if (b.n_seqs == 0) return hipSuccess;
-  const dim3 grid(budget >> c.scale_shift, n_kv_heads, b.n_seqs);
-  auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, s>>>(b, c, n_kv_heads, plan, budget);
+  const int blocks = budget >> c.scale_shift;
+  const dim3 grid(cdiv(budget, 128), n_kv_heads, b.n_seqs);
+  auto go = [&](auto one, auto two, auto four) {
+    const auto kernel = c.scale_shift == 5 ? one : (c.scale_shift == 6 ? two : four);
+    kernel<<<grid, 256, 0, s>>>(b, c, n_kv_heads, blocks, plan, budget);
     return hipGetLastError();
   };
-  if (head_dim == 128) return fp8 ? go(kv8_move_kernel<128, true>) : go(kv8_move_kernel<128, false>);
-  return fp8 ? go(kv8_move_kernel<64, true>) : go(kv8_move_kernel<64, false>);
+  if (head_dim == 128)
+    return fp8 ? go(kv8_move_kernel<128, true, 1>, kv8_move_kernel<128, true, 2>, kv8_move_kernel<128, true, 4>)
+               : go(kv8_move_kernel<128, false, 1>, kv8_move_kernel<128, false, 2>, kv8_move_kernel<128, false, 4>);
+  return fp8 ? go(kv8_move_kernel<64, true, 1>, kv8_move_kernel<64, true, 2>, kv8_move_kernel<64, true, 4>)
+             : go(kv8_move_kernel<64, false, 1>, kv8_move_kernel<64, false, 2>, kv8_move_kernel<64, false, 4>);
 }
 
 }  // namespace tri

@@ -5,6 +5,11 @@
 
 namespace tri {
 
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
+
 constexpr int kKv8LeastExp = -100;  // exponent of the smallest scale
 
 // First scale of (panel, head), and the first row's index in mass / stamp.

@@ -361,7 +361,10 @@ def test_select_and_move(name, page, stamp):
         max_seq = -(-max(c + n for c, n in zip(ctx, q)) // 64) * 64
         if max_seq > 10000 and d == 128:
             continue   # (the host's reference takes its time)
-        cache = make_cache(cfg, 3, max_seq, fmt, 32, page, seed=budget, stamp=stamp)
+        R = max(r for r in (32, 64, 128) if budget % r == 0 and (page or 64) % r == 0 or r == 32)
+        if not page and budget % 128 == 0:
+            R = 128
+        cache = make_cache(cfg, 3, max_seq, fmt, R, page, seed=budget, stamp=stamp)
         if stamp:   # positions in any order, as after an eviction
             cache.stamp.copy_(cache.stamp % (2 * max_seq))
         db = T.DeviceBatch(slot, ctx, q)
