@@ -302,13 +302,25 @@ typedef struct {
   float magnitude;      /* finite                                                 */
 } tri_rope_config;
 
+/* The configuration as the kernels take it, formed once and kept by the caller: every
+ * pair's turns per position, f_i / (2 pi).  Host only.  Errors: TRI_ERR_NULL,
+ * TRI_ERR_UNSUPPORTED (head_dim, layout, scaling), TRI_ERR_SHAPE (rotary_dim),
+ * TRI_ERR_RANGE (the numbers).                                                    */
+#define TRI_ROPE_MAX_PAIRS 128
+typedef struct {
+  int32_t head_dim, rotary_dim, layout;
+  float magnitude;
+  double turns[TRI_ROPE_MAX_PAIRS];
+} tri_rope_table;
+tri_status tri_rope_table_make(const tri_rope_config* cfg, tri_rope_table* table);
+
 /* y = x rotated.  x and y: device [n_tokens][n_heads][head_dim] of dtype (bf16 or
  * float32), tokens x_stride and y_stride elements apart (>= n_heads * head_dim:
  * the q and k heads of fused projection rows are one call); aligned to an
  * element, fastest where addresses and strides are multiples of 16 bytes and
  * rotary_dim of 32 bytes.  y may be x itself (same stride); any other overlap is
  * TRI_ERR_ALIAS.  pos: device int32 [n_tokens], any sign.                       */
-tri_status tri_rope(const tri_rope_config* cfg, const void* x, int64_t x_stride, void* y,
+tri_status tri_rope(const tri_rope_table* table, const void* x, int64_t x_stride, void* y,
                     int64_t y_stride, const int32_t* pos, int32_t n_tokens, int32_t n_heads,
                     int32_t dtype, void* stream);
 

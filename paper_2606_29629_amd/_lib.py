@@ -59,6 +59,11 @@ class RopeConfig(ctypes.Structure):
                [(n, ctypes.c_float) for n in ("base", "factor", "low", "high", "magnitude")]
 
 
+class RopeTable(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rotary_dim", "layout")] + \
+               [("magnitude", ctypes.c_float), ("turns", ctypes.c_double * 128)]
+
+
 class BatchStruct(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
                 ("max_q_len", ctypes.c_int32), ("max_ctx_len", ctypes.c_int32),
@@ -114,6 +119,7 @@ _FUNCS = {
     "tri_linear_workspace_size": (ctypes.c_int, [ctypes.c_int32] * 3 + [ctypes.c_void_p]),
     "tri_linear": (ctypes.c_int, [ctypes.c_void_p] * 3 + [ctypes.c_int32] * 3
                    + [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "tri_rope_table_make": (ctypes.c_int, [ctypes.c_void_p] * 2),
     "tri_rope": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                 ctypes.c_int64, ctypes.c_void_p] + [ctypes.c_int32] * 3
                  + [ctypes.c_void_p]),
@@ -358,55 +364,65 @@ def linear(a, b, out=None, workspace=None, stream=None):
 def make_rope(head_dim: int, rotary_dim: Optional[int] = None, base: float = 1e6,
               interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
               low: float = 1.0, high: float = 32.0, original_len: int = 0,
-              magnitude: float = 1.0) -> RopeConfig:
-    """RopeConfig of tri_rope; scaling: a key of ROPE_SCALING."""
+              magnitude: float = 1.0) -> RopeTable:
+    """What rope() takes, formed once (tri_rope_config, tri_rope_table_make); scaling: a key
+    of ROPE_SCALING."""
     if scaling not in ROPE_SCALING:
         raise ValueError(f"scaling {scaling!r}: one of {sorted(ROPE_SCALING)}")
-    return RopeConfig(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim),
-                      TRI_ROPE_INTERLEAVED if interleaved else TRI_ROPE_HALF,
-                      ROPE_SCALING[scaling], int(original_len), float(base), float(factor),
-                      float(low), float(high), float(magnitude))
+    cfg = RopeConfig(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim),
+                     TRI_ROPE_INTERLEAVED if interleaved else TRI_ROPE_HALF,
+                     ROPE_SCALING[scaling], int(original_len), float(base), float(factor),
+                     float(low), float(high), float(magnitude))
+    table = RopeTable()
+    _check(lib().tri_rope_table_make(ctypes.byref(cfg), ctypes.byref(table)), "tri_rope_table_make")
+    return table
 
 
-def _rows(x, what: str, last: int):
+def _rows(x, what: str, last: int) -> int:
     """Token stride of x [tokens, heads, last] whose heads are contiguous."""
-    if x.dim() != 3 or x.shape[2] != last or x.stride(2) != 1 or \
-            (x.shape[1] > 1 and x.stride(1) != last):
-        raise ValueError(f"{what}: [tokens, heads, {last}] with contiguous heads expected")
-    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * last)
+    if x.dim() == 3:
+        n, heads, d = x.shape
+        st = x.stride()
+        if d == last and st[2] == 1 and (heads <= 1 or st[1] == last):
+            return st[0] if n > 1 else max(st[0], heads * last)
+    raise ValueError(f"{what}: [tokens, heads, {last}] with contiguous heads expected")
 
 
-def _same_device(what: str, first, *others) -> None:
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"{what}: tensors on {first.device} and {t.device}")
-
-
-def _on_gpu(what: str, first, *others) -> None:
-    """The kernels follow plain addresses: every tensor of a call on the current GPU."""
+def _on_gpu(what: str, stream, first, *others) -> Optional[int]:
+    """The kernels follow plain addresses: every tensor of a call on the current GPU.
+    Returns the handle of `stream`, or of the current stream."""
     import torch
-    _same_device(what, first, *others)
-    if not first.is_cuda or first.device.index != torch.cuda.current_device():
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{what}: tensors on {first.device} and {t.device}")
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError(f"{what}: tensors on {first.device}, not on the current GPU")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    return getattr(stream, "cuda_stream", stream)
 
 
-def rope(cfg: RopeConfig, x, pos, out=None, stream=None):
+def rope(table: RopeTable, x, pos, out=None, stream=None):
     """x [tokens, heads, head_dim] (bf16 or float32, tokens any stride apart) with its
     heads rotated to int32 positions pos [tokens] (tri_rope); out=x: in place."""
     import torch
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if x.dtype not in (torch.bfloat16, torch.float32) or out.dtype != x.dtype:
+    f32 = x.dtype == torch.float32
+    if not f32 and x.dtype != torch.bfloat16 or out.dtype != x.dtype:
         raise ValueError(f"rope: bf16 or float32 in and out, got {x.dtype} and {out.dtype}")
-    if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() != x.shape[0]:
+    xs, ys = _rows(x, "rope: x", table.head_dim), _rows(out, "rope: out", table.head_dim)
+    n, heads, _ = x.shape
+    if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() != n:
         raise ValueError("rope: pos is a contiguous int32 [tokens]")
     if out.shape != x.shape:
         raise ValueError(f"rope: out {tuple(out.shape)}, x {tuple(x.shape)}")
-    _on_gpu("rope", x, pos, out)
-    xs, ys = _rows(x, "rope: x", cfg.head_dim), _rows(out, "rope: out", cfg.head_dim)
-    _check(lib().tri_rope(ctypes.byref(cfg), _ptr(x), xs, _ptr(out), ys, _ptr(pos), x.shape[0],
-                          x.shape[1], TRI_F32 if x.dtype == torch.float32 else TRI_BF16,
-                          _stream(stream)), "tri_rope")
+    stream = _on_gpu("rope", stream, x, pos, out)
+    st = lib().tri_rope(ctypes.byref(table), x.data_ptr(), xs, out.data_ptr(), ys, pos.data_ptr(),
+                        n, heads, f32, stream)
+    if st:
+        raise TriError(st, "tri_rope")
     return out
 
 
@@ -441,7 +457,8 @@ class KV8Cache:
         tensors = (k, v, k_scale, v_scale, mass, stamp, block_table)
         if not all(t is None or t.is_contiguous() for t in tensors):
             raise ValueError("KV8Cache: contiguous tensors expected")
-        _same_device("KV8Cache", *tensors)
+        if any(t is not None and t.device != k.device for t in tensors):
+            raise ValueError("KV8Cache: tensors on one device expected")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.mass, self.stamp, self.block_table = mass, stamp, block_table
         self.scale_rows, self.head_dim, self.n_kv_heads = int(scale_rows), int(k.shape[3]), int(heads)
@@ -451,6 +468,7 @@ class KV8Cache:
         self._struct = KV8CacheStruct(*[_ptr(t) for t in tensors[:6]], self.n_slots, self.max_seq,
                                       _ptr(block_table), int(rows) if paged else 0,
                                       int(panels) if paged else 0, formats[k.dtype], self.scale_rows)
+        self._ref = ctypes.byref(self._struct)  # (the tensors of a cache do not change)
 
     @classmethod
     def empty(cls, cfg: LayerConfig, n_slots: int, max_seq: int, format: str = "int8",
@@ -475,34 +493,39 @@ class KV8Cache:
         return self._struct
 
 
-def _kv8(what, cfg, cache, batch, *tensors):
-    if (cfg.n_kv_heads, cfg.head_dim) != (cache.n_kv_heads, cache.head_dim):
+def _kv8(what, cfg, cache, batch, stream, *tensors):
+    """The first arguments of a call on an 8-bit cache, and its stream."""
+    if cfg.n_kv_heads != cache.n_kv_heads or cfg.head_dim != cache.head_dim:
         raise ValueError(f"{what}: the cache has {cache.n_kv_heads} heads of {cache.head_dim}, "
                          f"the layer {cfg.n_kv_heads} of {cfg.head_dim}")
-    _on_gpu(what, cache.k, batch.slot, *tensors)
-    return ctypes.byref(cfg), ctypes.byref(cache.struct()), ctypes.byref(batch.struct())
+    return (ctypes.byref(cfg), cache._ref, ctypes.byref(batch.struct()),
+            _on_gpu(what, stream, cache.k, batch.slot, *tensors))
 
 
 def kv8_append(cfg, cache: KV8Cache, batch, k_new, v_new, stream=None) -> None:
     """The batch's new keys (rotated) and values [tokens, Hkv, D] (bf16, tokens any one
     stride apart) into the 8-bit cache (tri_kv8_append)."""
     import torch
-    stride = _rows(k_new, "kv8_append: k_new", cfg.head_dim)
-    shape = (batch.n_tokens, cfg.n_kv_heads, cfg.head_dim)
-    if tuple(k_new.shape) != shape or tuple(v_new.shape) != shape or \
-            _rows(v_new, "kv8_append: v_new", cfg.head_dim) != stride:
-        raise ValueError(f"kv8_append: k_new and v_new are {shape} with one token stride")
+    d = cfg.head_dim
+    stride = _rows(k_new, "kv8_append: k_new", d)
+    n, heads, _ = k_new.shape
+    if n != batch.n_tokens or heads != cfg.n_kv_heads or v_new.shape != k_new.shape or \
+            _rows(v_new, "kv8_append: v_new", d) != stride:
+        raise ValueError(f"kv8_append: k_new and v_new are [{batch.n_tokens}, {cfg.n_kv_heads}, {d}] "
+                         "with one token stride")
     if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
         raise ValueError("kv8_append: k_new and v_new are bf16")
-    _check(lib().tri_kv8_append(*_kv8("kv8_append", cfg, cache, batch, k_new, v_new), _ptr(k_new),
-                                _ptr(v_new), stride, _stream(stream)), "tri_kv8_append")
+    c, kv, b, stream = _kv8("kv8_append", cfg, cache, batch, stream, k_new, v_new)
+    st = lib().tri_kv8_append(c, kv, b, k_new.data_ptr(), v_new.data_ptr(), stride, stream)
+    if st:
+        raise TriError(st, "tri_kv8_append")
 
 
 def kv8_attention_workspace_size(cfg, cache: KV8Cache, batch) -> int:
     n = ctypes.c_size_t()
     _check(lib().tri_kv8_attention_workspace_size(
-        ctypes.byref(cfg), ctypes.byref(cache.struct()), ctypes.byref(batch.struct()),
-        ctypes.byref(n)), "tri_kv8_attention_workspace_size")
+        ctypes.byref(cfg), cache._ref, ctypes.byref(batch.struct()), ctypes.byref(n)),
+        "tri_kv8_attention_workspace_size")
     return n.value
 
 
@@ -510,30 +533,37 @@ def kv8_attention(cfg, cache: KV8Cache, batch, q, out=None, workspace=None, stre
     """Causal attention of q [tokens, Hq, D] (bf16, tokens any stride apart) over the 8-bit
     cache, adding up cache.mass where it has one (tri_kv8_attention); returns (out, workspace)."""
     import torch
-    shape = (batch.n_tokens, cfg.n_q_heads, cfg.head_dim)
-    if tuple(q.shape) != shape or q.dtype != torch.bfloat16:
-        raise ValueError(f"kv8_attention: q is bf16 {shape}")
     stride = _rows(q, "kv8_attention: q", cfg.head_dim)
+    n, heads, _ = q.shape
+    if n != batch.n_tokens or heads != cfg.n_q_heads or q.dtype != torch.bfloat16:
+        raise ValueError(f"kv8_attention: q is bf16 [{batch.n_tokens}, {cfg.n_q_heads}, {cfg.head_dim}]")
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
-    if tuple(out.shape) != shape or out.dtype != q.dtype or not out.is_contiguous():
-        raise ValueError(f"kv8_attention: out is contiguous bf16 {shape}")
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError(f"kv8_attention: out is contiguous bf16 {tuple(q.shape)}")
     if workspace is None:
         workspace = torch.empty(kv8_attention_workspace_size(cfg, cache, batch),
                                 dtype=torch.uint8, device=q.device)
-    args = _kv8("kv8_attention", cfg, cache, batch, q, out, workspace)
-    _check(lib().tri_kv8_attention(*args, _ptr(q), stride, _ptr(out), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream(stream)),
-           "tri_kv8_attention")
+    c, kv, b, stream = _kv8("kv8_attention", cfg, cache, batch, stream, q, out, workspace)
+    st = lib().tri_kv8_attention(c, kv, b, q.data_ptr(), stride, out.data_ptr(), workspace.data_ptr(),
+                                 workspace.nbytes, stream)
+    if st:
+        raise TriError(st, "tri_kv8_attention")
     return out, workspace
 
 
 def kv8_select_workspace_size(cfg, cache: KV8Cache, batch, budget: int) -> int:
     n = ctypes.c_size_t()
     _check(lib().tri_kv8_select_workspace_size(
-        ctypes.byref(cfg), ctypes.byref(cache.struct()), ctypes.byref(batch.struct()), int(budget),
-        ctypes.byref(n)), "tri_kv8_select_workspace_size")
+        ctypes.byref(cfg), cache._ref, ctypes.byref(batch.struct()), int(budget), ctypes.byref(n)),
+        "tri_kv8_select_workspace_size")
     return n.value
+
+
+def _plan(what, plan, n_seqs: int, heads: int, budget: int) -> None:
+    import torch
+    if plan.dtype != torch.int32 or plan.shape != (n_seqs, heads, budget) or not plan.is_contiguous():
+        raise ValueError(f"{what}: plan is a contiguous int32 {(n_seqs, heads, budget)}")
 
 
 def kv8_select(cfg, cache: KV8Cache, batch, budget: int, n_first: int = 0, n_recent: int = 0,
@@ -541,36 +571,34 @@ def kv8_select(cfg, cache: KV8Cache, batch, budget: int, n_first: int = 0, n_rec
     """Which rows of the batch's sequences (ctx_len + q_len each) stay within budget
     (tri_kv8_select); returns (plan [n_seqs, Hkv, budget], new_len [n_seqs]), int32."""
     import torch
-    shape = (batch.n_seqs, cfg.n_kv_heads, int(budget))
+    n = batch.n_seqs
     if plan is None:
-        plan = torch.empty(shape, dtype=torch.int32, device=cache.k.device)
+        plan = torch.empty((n, cfg.n_kv_heads, budget), dtype=torch.int32, device=cache.k.device)
     if new_len is None:
-        new_len = torch.empty(batch.n_seqs, dtype=torch.int32, device=cache.k.device)
-    _plan("kv8_select", plan, shape)
-    if new_len.dtype != torch.int32 or new_len.numel() != batch.n_seqs or not new_len.is_contiguous():
-        raise ValueError(f"kv8_select: new_len is a contiguous int32 [{batch.n_seqs}]")
-    args = _kv8("kv8_select", cfg, cache, batch, plan, new_len, workspace)
+        new_len = torch.empty(n, dtype=torch.int32, device=cache.k.device)
+    _plan("kv8_select", plan, n, cfg.n_kv_heads, budget)
+    if new_len.dtype != torch.int32 or new_len.numel() != n or not new_len.is_contiguous():
+        raise ValueError(f"kv8_select: new_len is a contiguous int32 [{n}]")
     if workspace is None and batch.max_ctx_len + batch.max_q_len > 16384:  # (else none is needed)
         workspace = torch.empty(kv8_select_workspace_size(cfg, cache, batch, budget),
                                 dtype=torch.uint8, device=plan.device)
-    _check(lib().tri_kv8_select(*args, int(budget), int(n_first), int(n_recent), _ptr(plan),
-                                _ptr(new_len), _ptr(workspace),
-                                0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                _stream(stream)), "tri_kv8_select")
+    c, kv, b, stream = _kv8("kv8_select", cfg, cache, batch, stream, plan, new_len, workspace)
+    st = lib().tri_kv8_select(c, kv, b, budget, n_first, n_recent, plan.data_ptr(),
+                              new_len.data_ptr(), _ptr(workspace),
+                              0 if workspace is None else workspace.nbytes, stream)
+    if st:
+        raise TriError(st, "tri_kv8_select")
     return plan, new_len
-
-
-def _plan(what, plan, shape):
-    import torch
-    if plan.dtype != torch.int32 or tuple(plan.shape) != tuple(shape) or not plan.is_contiguous():
-        raise ValueError(f"{what}: plan is a contiguous int32 {tuple(shape)}")
 
 
 def kv8_move(cfg, cache: KV8Cache, batch, plan, stream=None) -> None:
     """Rows of the batch's sequences to the places of a kv8_select plan (tri_kv8_move)."""
-    _plan("kv8_move", plan, (batch.n_seqs, cfg.n_kv_heads, plan.shape[-1]))
-    _check(lib().tri_kv8_move(*_kv8("kv8_move", cfg, cache, batch, plan), _ptr(plan),
-                              int(plan.shape[-1]), _stream(stream)), "tri_kv8_move")
+    budget = plan.shape[-1] if plan.dim() else 0
+    _plan("kv8_move", plan, batch.n_seqs, cfg.n_kv_heads, budget)
+    c, kv, b, stream = _kv8("kv8_move", cfg, cache, batch, stream, plan)
+    st = lib().tri_kv8_move(c, kv, b, plan.data_ptr(), budget, stream)
+    if st:
+        raise TriError(st, "tri_kv8_move")
 
 
 def moe_route(cfg, h2_f32, w_router, idx, w, stream=None) -> None:

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/tri.h"
 #include "plan.hpp"
 
 namespace tri {
@@ -195,14 +196,8 @@ hipError_t launch_attn_decode_combine(const float* part, void* out, const BatchD
                                       const KvDev& kv, int n_q_heads, int n_kv_heads,
                                       int head_dim, hipStream_t s);
 
-// Rotary positions (tri_rope): per pair its turns per position, f / 2 pi.
-constexpr int kRopeMaxPairs = 128;
-struct RopeDev {
-  double turns[kRopeMaxPairs];
-  int rot, head_dim, n_heads;
-  float magnitude;
-};
-hipError_t launch_rope(const RopeDev& r, bool interleaved, const void* x, int64_t xs, void* y,
+// Rotary positions (tri_rope).
+hipError_t launch_rope(const tri_rope_table& r, int n_heads, const void* x, int64_t xs, void* y,
                        int64_t ys, const int32_t* pos, int n_tokens, bool f32, hipStream_t s);
 
 // 8-bit KV cache: rows addressed as in KvDev, one byte per value, one scale per head

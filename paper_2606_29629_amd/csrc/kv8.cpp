@@ -93,13 +93,22 @@ size_t extent(int64_t rows, int64_t width, int64_t stride, int size) {
   return (size_t)((rows - 1) * stride + width) * size;
 }
 
-tri_status check_rope(const tri_rope_config* c) {
-  if (!c) return TRI_ERR_NULL;
-  if (c->head_dim < 2 || c->head_dim > 2 * kRopeMaxPairs || c->head_dim % 2) return TRI_ERR_UNSUPPORTED;
+// What a configuration and its table share.
+template <typename C>
+tri_status check_rope_dims(const C* c) {
+  if (c->head_dim < 2 || c->head_dim > 2 * TRI_ROPE_MAX_PAIRS || c->head_dim % 2)
+    return TRI_ERR_UNSUPPORTED;
   if (c->rotary_dim < 2 || c->rotary_dim > c->head_dim || c->rotary_dim % 2) return TRI_ERR_SHAPE;
   if (c->layout != TRI_ROPE_HALF && c->layout != TRI_ROPE_INTERLEAVED) return TRI_ERR_UNSUPPORTED;
+  return isfinite(c->magnitude) ? TRI_OK : TRI_ERR_RANGE;
+}
+
+tri_status check_rope(const tri_rope_config* c) {
+  if (!c) return TRI_ERR_NULL;
+  const tri_status st = check_rope_dims(c);
+  if (st != TRI_OK) return st;
   if (c->scaling < TRI_ROPE_PLAIN || c->scaling > TRI_ROPE_INDEX) return TRI_ERR_UNSUPPORTED;
-  if (!(c->base > 0.f) || !isfinite(c->base) || !isfinite(c->magnitude)) return TRI_ERR_RANGE;
+  if (!(c->base > 0.f) || !isfinite(c->base)) return TRI_ERR_RANGE;
   if (c->scaling != TRI_ROPE_PLAIN && (!(c->factor > 0.f) || !isfinite(c->factor))) return TRI_ERR_RANGE;
   if (c->scaling == TRI_ROPE_TURNS || c->scaling == TRI_ROPE_INDEX) {
     if (c->original_len <= 0 || !(c->low > 0.f) || !(c->high > c->low) || !isfinite(c->high))
@@ -110,12 +119,7 @@ tri_status check_rope(const tri_rope_config* c) {
 }
 
 // Every pair's turns per position, f / 2 pi (the formulas of tri_rope_config).
-RopeDev rope_dev(const tri_rope_config* c, int n_heads) {
-  RopeDev r{};
-  r.rot = c->rotary_dim;
-  r.head_dim = c->head_dim;
-  r.n_heads = n_heads;
-  r.magnitude = c->magnitude;
+void rope_turns(const tri_rope_config* c, double* turns) {
   const double two_pi = 6.283185307179586, n = c->rotary_dim, factor = c->factor;
   double base = c->base;
   if (c->scaling == TRI_ROPE_BASE && c->rotary_dim > 2) base *= pow(factor, n / (n - 2));
@@ -138,19 +142,28 @@ RopeDev rope_dev(const tri_rope_config* c, int n_heads) {
       const double u = std::min(1.0, std::max(0.0, (i - lo) / std::max(hi - lo, 0.001)));
       f = w * (1 - u) + w / factor * u;
     }
-    r.turns[i] = f / two_pi;
+    turns[i] = f / two_pi;
   }
-  return r;
 }
 
 }  // namespace
 
 extern "C" {
 
-tri_status tri_rope(const tri_rope_config* cfg, const void* x, int64_t x_stride, void* y,
+tri_status tri_rope_table_make(const tri_rope_config* cfg, tri_rope_table* table) {
+  if (!table) return TRI_ERR_NULL;
+  const tri_status st = check_rope(cfg);
+  if (st != TRI_OK) return st;
+  *table = tri_rope_table{cfg->head_dim, cfg->rotary_dim, cfg->layout, cfg->magnitude, {}};
+  rope_turns(cfg, table->turns);
+  return TRI_OK;
+}
+
+tri_status tri_rope(const tri_rope_table* cfg, const void* x, int64_t x_stride, void* y,
                     int64_t y_stride, const int32_t* pos, int32_t n_tokens, int32_t n_heads,
                     int32_t dtype, void* stream) {
-  tri_status st = check_rope(cfg);
+  if (!cfg) return TRI_ERR_NULL;
+  tri_status st = check_rope_dims(cfg);
   if (st != TRI_OK) return st;
   if (dtype != TRI_BF16 && dtype != TRI_F32) return TRI_ERR_UNSUPPORTED;
   if (n_tokens < 0 || n_heads < 0) return TRI_ERR_SHAPE;
@@ -165,8 +178,8 @@ tri_status tri_rope(const tri_rope_config* cfg, const void* x, int64_t x_stride,
       overlaps(x, extent(n_tokens, width, x_stride, size), y,
                extent(n_tokens, width, y_stride, size)))
     return TRI_ERR_ALIAS;
-  TRI_HIP(launch_rope(rope_dev(cfg, n_heads), cfg->layout == TRI_ROPE_INTERLEAVED, x, x_stride, y,
-                      y_stride, pos, n_tokens, dtype == TRI_F32, (hipStream_t)stream));
+  TRI_HIP(launch_rope(*cfg, n_heads, x, x_stride, y, y_stride, pos, n_tokens, dtype == TRI_F32,
+                      (hipStream_t)stream));
   return TRI_OK;
 }
 

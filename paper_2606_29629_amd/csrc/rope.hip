@@ -16,11 +16,11 @@
 namespace tri {
 
 template <typename T, int V, bool INTERLEAVED>
-__global__ __launch_bounds__(256) void rope_kernel(RopeDev r, const T* x, int64_t xs, T* y,
+__global__ __launch_bounds__(256) void rope_kernel(tri_rope_table r, int n_heads, const T* x, int64_t xs, T* y,
                                                    int64_t ys, const int32_t* __restrict__ pos,
                                                    int n_tokens, int per_wg, int copy_tail) {
   extern __shared__ float2 table[];  // [per_wg][rot / 2]
-  const int half = r.rot / 2;
+  const int rot = r.rotary_dim, half = rot / 2;
   const int t0 = blockIdx.x * per_wg, nt = min(per_wg, n_tokens - t0);
   for (int i = threadIdx.x; i < nt * half; i += blockDim.x) {
     const int t = i / half;
@@ -33,15 +33,15 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeDev r, const T* x, int64_
   typedef T Vec __attribute__((ext_vector_type(V)));
   // items of a head: `half / V` of pairs, then the unrotated rest in pieces of V
   const int pairs = half / V;
-  const int per_head = pairs + (copy_tail ? (r.head_dim - r.rot) / V : 0);
-  const int per_tok = per_head * r.n_heads;
+  const int per_head = pairs + (copy_tail ? (r.head_dim - rot) / V : 0);
+  const int per_tok = per_head * n_heads;
   for (int i = threadIdx.x; i < nt * per_tok; i += blockDim.x) {
     const int t = i / per_tok, k = i - t * per_tok;
     const int h = k / per_head, j = k - h * per_head;
     const T* xp = x + (int64_t)(t0 + t) * xs + h * r.head_dim;
     T* yp = y + (int64_t)(t0 + t) * ys + h * r.head_dim;
     if (j >= pairs) {
-      const int d = r.rot + (j - pairs) * V;
+      const int d = rot + (j - pairs) * V;
       *(Vec*)(yp + d) = *(const Vec*)(xp + d);
       continue;
     }
@@ -78,17 +78,19 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeDev r, const T* x, int64_
 }
 
 template <typename T>
-static hipError_t run_rope(const RopeDev& r, bool interleaved, const void* x, int64_t xs, void* y,
+static hipError_t run_rope(const tri_rope_table& r, int n_heads, const void* x, int64_t xs, void* y,
                            int64_t ys, const int32_t* pos, int n_tokens, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
-  const bool wide = r.rot % (2 * V) == 0 && r.head_dim % V == 0 && xs % V == 0 && ys % V == 0 &&
+  const int rot = r.rotary_dim;
+  const bool interleaved = r.layout == TRI_ROPE_INTERLEAVED;
+  const bool wide = rot % (2 * V) == 0 && r.head_dim % V == 0 && xs % V == 0 && ys % V == 0 &&
                     ((uintptr_t)x | (uintptr_t)y) % 16 == 0;
-  const int copy_tail = x != y && r.rot < r.head_dim;
-  const int items = r.n_heads * (r.rot / 2 + (copy_tail ? r.head_dim - r.rot : 0)) / (wide ? V : 1);
+  const int copy_tail = x != y && rot < r.head_dim;
+  const int items = n_heads * (rot / 2 + (copy_tail ? r.head_dim - rot : 0)) / (wide ? V : 1);
   const int per_wg = std::max(1, std::min(8, 512 / std::max(1, items)));
-  const size_t smem = (size_t)per_wg * (r.rot / 2) * sizeof(float2);
+  const size_t smem = (size_t)per_wg * (rot / 2) * sizeof(float2);
   auto go = [&](auto kernel) {
-    kernel<<<cdiv(n_tokens, per_wg), 256, smem, s>>>(r, (const T*)x, xs, (T*)y, ys, pos, n_tokens,
+    kernel<<<cdiv(n_tokens, per_wg), 256, smem, s>>>(r, n_heads, (const T*)x, xs, (T*)y, ys, pos, n_tokens,
                                                      per_wg, copy_tail);
     return hipGetLastError();
   };
@@ -96,10 +98,10 @@ static hipError_t run_rope(const RopeDev& r, bool interleaved, const void* x, in
   return interleaved ? go(rope_kernel<T, 1, true>) : go(rope_kernel<T, 1, false>);
 }
 
-hipError_t launch_rope(const RopeDev& r, bool interleaved, const void* x, int64_t xs, void* y,
+hipError_t launch_rope(const tri_rope_table& r, int n_heads, const void* x, int64_t xs, void* y,
                        int64_t ys, const int32_t* pos, int n_tokens, bool f32, hipStream_t s) {
-  return f32 ? run_rope<float>(r, interleaved, x, xs, y, ys, pos, n_tokens, s)
-             : run_rope<bf16>(r, interleaved, x, xs, y, ys, pos, n_tokens, s);
+  return f32 ? run_rope<float>(r, n_heads, x, xs, y, ys, pos, n_tokens, s)
+             : run_rope<bf16>(r, n_heads, x, xs, y, ys, pos, n_tokens, s);
 }
 
 }  // namespace tri

@@ -26,7 +26,8 @@ def lib():
     return T.lib()
 
 
-STRUCTS = {"tri_kv8_cache": T.KV8CacheStruct, "tri_rope_config": T.RopeConfig}
+STRUCTS = {"tri_kv8_cache": T.KV8CacheStruct, "tri_rope_config": T.RopeConfig,
+           "tri_rope_table": T.RopeTable}
 
 
 def test_struct_layout_matches_header():
@@ -181,25 +182,54 @@ def rope(lib, c=None, x=FAKE, xs=512, y=FAKE + (1 << 20), ys=512, pos=FAKE + (2 
                         dtype, None)
 
 
-def test_rope_refusals(lib):
-    assert rope(lib, c=T.make_rope(258)) == T.TRI_ERR_UNSUPPORTED
-    assert rope(lib, c=T.make_rope(127)) == T.TRI_ERR_UNSUPPORTED
+def rope_status(*args, **kw):
+    with pytest.raises(T.TriError) as e:
+        T.make_rope(*args, **kw)
+    return e.value.status
+
+
+def test_rope_table_refusals(lib):
+    assert rope_status(258) == T.TRI_ERR_UNSUPPORTED
+    assert rope_status(127) == T.TRI_ERR_UNSUPPORTED
     for r in (0, 1, 63, 130):
-        assert rope(lib, c=T.make_rope(128, rotary_dim=r)) == T.TRI_ERR_SHAPE
-    c = T.make_rope(128)
-    c.layout = 2
-    assert rope(lib, c=c) == T.TRI_ERR_UNSUPPORTED
-    c = T.make_rope(128)
-    c.scaling = 5
-    assert rope(lib, c=c) == T.TRI_ERR_UNSUPPORTED
-    assert rope(lib, c=T.make_rope(128, base=0.0)) == T.TRI_ERR_RANGE
-    assert rope(lib, c=T.make_rope(128, magnitude=math.inf)) == T.TRI_ERR_RANGE
-    assert rope(lib, c=T.make_rope(128, scaling="linear", factor=0.0)) == T.TRI_ERR_RANGE
+        assert rope_status(128, rotary_dim=r) == T.TRI_ERR_SHAPE
+    table = T.RopeTable()
+    for name, status in (("layout", T.TRI_ERR_UNSUPPORTED), ("scaling", T.TRI_ERR_UNSUPPORTED)):
+        c = T.RopeConfig(128, 128, 0, 0, 0, 1e6, 1.0, 1.0, 32.0, 1.0)
+        setattr(c, name, 5)
+        assert lib.tri_rope_table_make(ctypes.byref(c), ctypes.byref(table)) == status
+    assert lib.tri_rope_table_make(None, ctypes.byref(table)) == T.TRI_ERR_NULL
+    assert lib.tri_rope_table_make(ctypes.byref(c), None) == T.TRI_ERR_NULL
+    assert rope_status(128, base=0.0) == T.TRI_ERR_RANGE
+    assert rope_status(128, magnitude=math.inf) == T.TRI_ERR_RANGE
+    assert rope_status(128, scaling="linear", factor=0.0) == T.TRI_ERR_RANGE
     for kw in (dict(original_len=0), dict(original_len=4096, low=0.0),
                dict(original_len=4096, low=2.0, high=2.0)):
         for scaling in ("turns", "index"):
-            assert rope(lib, c=T.make_rope(128, scaling=scaling, **kw)) == T.TRI_ERR_RANGE
-    assert rope(lib, c=T.make_rope(128, scaling="index", base=1.0, original_len=9)) == T.TRI_ERR_RANGE
+            assert rope_status(128, scaling=scaling, **kw) == T.TRI_ERR_RANGE
+    assert rope_status(128, scaling="index", base=1.0, original_len=9) == T.TRI_ERR_RANGE
+    with pytest.raises(ValueError):
+        T.make_rope(128, scaling="cubic")
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(scaling="linear", factor=3.0),
+                                dict(scaling="base", factor=8.0),
+                                dict(scaling="turns", factor=8.0, original_len=8192, high=4.0),
+                                dict(scaling="index", factor=40.0, original_len=4096)])
+@pytest.mark.parametrize("rotary", [128, 20, 2])
+def test_rope_table_is_the_formulas(lib, kw, rotary):
+    table = T.make_rope(128, rotary, base=1e4, **kw)
+    want = kv8_ref.rope_freqs(rotary, 1e4, **kw) / (2 * math.pi)
+    assert np.allclose(table.turns[:rotary // 2], want, rtol=1e-12, atol=0)
+
+
+def test_rope_refusals(lib):
+    assert lib.tri_rope(None, FAKE, 512, FAKE, 512, FAKE, 1, 1, 0, None) == T.TRI_ERR_NULL
+    for name, v, status in (("head_dim", 300, T.TRI_ERR_UNSUPPORTED), ("rotary_dim", 0, T.TRI_ERR_SHAPE),
+                            ("layout", 2, T.TRI_ERR_UNSUPPORTED), ("magnitude", math.nan, T.TRI_ERR_RANGE)):
+        c = T.make_rope(128)
+        setattr(c, name, v)
+        assert rope(lib, c=c) == status
     assert rope(lib, dtype=2) == T.TRI_ERR_UNSUPPORTED
     assert rope(lib, xs=511) == T.TRI_ERR_SHAPE
     assert rope(lib, tokens=-1) == T.TRI_ERR_SHAPE
@@ -209,8 +239,6 @@ def test_rope_refusals(lib):
     assert rope(lib, y=FAKE + 256) == T.TRI_ERR_ALIAS
     assert rope(lib, y=FAKE, ys=520) == T.TRI_ERR_ALIAS                      # itself, another stride
     assert rope(lib, tokens=0, x=None) == T.TRI_OK
-    with pytest.raises(ValueError):
-        T.make_rope(128, scaling="cubic")
 
 
 def test_binding_refuses_before_the_call():
