@@ -74,62 +74,62 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, 
   if (kt_lo >= kt_hi) return;  // (the merge skips an empty split)
 
   const int prows = c.kv.panel_rows(), spp = c.scales_per_panel();
-  struct Place {
-    int panel, prow;
-  };
-  auto place = [&](int kt) {
-    Place p{sl, kt * kKeys8};
-    if (PAGED && kt < nkt) p.panel = kv_panel(c.kv, sl, kt * kKeys8, p.prow);
-    return p;
-  };
   int st_row[NL], st_chunk[NL];
 #pragma unroll
   for (int j = 0; j < NL; ++j) stage_place<D>(tid + 256 * j, st_row[j], st_chunk[j]);
   u32x4 kraw[NL], vraw[NL];
   float ks_next[2], vs_next[2];  // the scales of the tile in kraw, vraw
+  // A tile's codes and scales: contiguous, at an offset from the head's first row; paged,
+  // from its page.  Rows past the end (and tiles past the last) read as zero.
+  auto rsrc = [&](const uint8_t* base, int panel, int rows) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + ((int64_t)panel * Hkv + h) * prows * D), (short)0,
+                                             rows * D, 0x00020000);
+  };
+  const auto rk0 = rsrc(c.k, sl, PAGED ? 0 : kv_len), rv0 = rsrc(c.v, sl, PAGED ? 0 : kv_len);
+  const int64_t scale0 = ((int64_t)sl * Hkv + h) * spp;
   auto gload = [&](int kt) {
-    Place p = place(kt);
-    int live = min(kKeys8, kv_len - kt * kKeys8);
-    if (p.panel < 0 || live <= 0) live = p.panel = p.prow = 0;
-    const int64_t head = (int64_t)p.panel * Hkv + h;
-    const int64_t at = (head * prows + p.prow) * D;
-    const auto rk = __builtin_amdgcn_make_buffer_rsrc((void*)(c.k + at), (short)0, live * D, 0x00020000);
-    const auto rv = __builtin_amdgcn_make_buffer_rsrc((void*)(c.v + at), (short)0, live * D, 0x00020000);
+    auto rk = rk0, rv = rv0;
+    int first = min(kt, nkt - 1) * kKeys8;  // row within the panel
+    int64_t sa = scale0;
+    const int live = kv_len - first;
+    if constexpr (PAGED) {
+      int panel = kv_panel(c.kv, sl, first, first);
+      const int rows = panel < 0 ? 0 : min(prows, first + live);
+      panel = max(panel, 0);
+      rk = rsrc(c.k, panel, rows);
+      rv = rsrc(c.v, panel, rows);
+      sa = ((int64_t)panel * Hkv + h) * spp;
+    }
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
       const int off = st_row[j] * D + st_chunk[j] * 16;
-      kraw[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
-      vraw[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
+      kraw[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, first * D, 0));
+      vraw[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, first * D, 0));
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const bool seen = 32 * u < live;  // (scales of rows past the end are not looked at)
-      const int64_t sa = head * spp + ((p.prow + (seen ? 32 * u : 0)) >> c.scale_shift);
-      ks_next[u] = seen ? c.k_scale[sa] : 1.f;
-      vs_next[u] = seen ? c.v_scale[sa] : 1.f;
+    for (int u = 0; u < 2; ++u) {  // (a block wholly past the end takes the other's)
+      const int64_t at = sa + ((first + (32 * u < live ? 32 * u : 0)) >> c.scale_shift);
+      ks_next[u] = c.k_scale[at];
+      vs_next[u] = c.v_scale[at];
     }
   };
   float ks[2], vs[2];
-  auto convert = [&](int buf) {
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int r = st_row[j], c0 = 2 * st_chunk[j];
-      f16* kd = sk[buf] + r * D;
-      f16* vd = sv[buf] + r * D;
-      const int p0 = kv_chunk<D>(c0, r) * 8, p1 = kv_chunk<D>(c0 + 1, r) * 8;
-      *(f16x8*)(kd + p0) = codes_to_f16<FP8>(kraw[j][0], kraw[j][1]);
-      *(f16x8*)(kd + p1) = codes_to_f16<FP8>(kraw[j][2], kraw[j][3]);
-      *(f16x8*)(vd + p0) = codes_to_f16<FP8>(vraw[j][0], vraw[j][1]);
-      *(f16x8*)(vd + p1) = codes_to_f16<FP8>(vraw[j][2], vraw[j][3]);
-    }
+  // Eight codes of a thread's share of the tile in kraw, vraw into LDS: unit u of 4 NL.
+  auto convert = [&](auto unit, int buf) {
+    constexpr int j = decltype(unit)::value >> 2, is_v = (decltype(unit)::value >> 1) & 1,
+                  half = decltype(unit)::value & 1;
+    const int r = st_row[j];
+    f16* dst = (is_v ? sv : sk)[buf] + r * D + kv_chunk<D>(2 * st_chunk[j] + half, r) * 8;
+    const u32x4 x = is_v ? vraw[j] : kraw[j];
+    *(f16x8*)dst = codes_to_f16<FP8>(x[2 * half], x[2 * half + 1]);
   };
+  auto convert_all = [&](int buf) { each<4 * NL>([&](auto u) { convert(u, buf); }); };
 
   // This lane's query row (rows past the end repeat the last one and are not written).
   const int row = row0 + wave * 32 + lr, rc = min(row, rows - 1);
   const int tok = rc / G, hq = h * G + rc - tok * G;
   const int qpos = ctx + tok;
-  const int wave_lo = ctx + min(row0 + wave * 32, rows - 1) / G;  // first and last token of the wave
-  const int wave_hi = ctx + min(row0 + wave * 32 + 31, rows - 1) / G;
+  const int wave_lo = ctx + min(row0 + wave * 32, rows - 1) / G;  // the wave's first token
   f16x8 qf[DS];
   float score_scale;
   gload(kt_lo);
@@ -148,116 +148,120 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, 
   for (int d = 0; d < DB; ++d) oacc[d] = f32x16{0.f};
   float m_run = -INFINITY, l_run = 0.f;  // log2 units
 
-  convert(0);
+  convert_all(0);
   ks[0] = ks_next[0], ks[1] = ks_next[1], vs[0] = vs_next[0], vs[1] = vs_next[1];
-  if (kt_lo + 1 < kt_hi) gload(kt_lo + 1);
+  gload(kt_lo + 1);
 
+  // Key tile kt from buffer `buf`.  Both products have other work under them: the first the
+  // conversion of the next tile, the second the weights of its next 16 keys.
   auto step = [&](int kt, auto buf) {
+    constexpr int other = 1 - decltype(buf)::value;
     __syncthreads();  // tile kt is in LDS; every wave is done with tile kt - 1
-    float ks_after[2] = {ks_next[0], ks_next[1]}, vs_after[2] = {vs_next[0], vs_next[1]};
-    if (kt + 1 < kt_hi) convert(1 - decltype(buf)::value);
-    if (kt + 2 < kt_hi) gload(kt + 2);
     const f16* kb_lds = sk[decltype(buf)::value];
     const f16* vb = sv[decltype(buf)::value];
     const int key0 = kt * kKeys8;
-    if (key0 <= wave_hi) {  // (else no key of this tile is visible to this wave)
-      constexpr int KLA = 3;
-      f32x16 sacc[2] = {f32x16{0.f}, f32x16{0.f}};
-      f16x8 kf[KLA + 1][2];
-      auto kread = [&](int t, f16x8 (&dst)[2]) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const int key = kb * 32 + lr;
-          dst[kb] = *(const f16x8*)&kb_lds[key * D + kv_chunk<D>(2 * t + lg, key) * 8];
-        }
-      };
-#pragma unroll
-      for (int t = 0; t < KLA && t < DS; ++t) kread(t, kf[t]);
-#pragma unroll
-      for (int t = 0; t < DS; ++t) {
-        if (t + KLA < DS) kread(t + KLA, kf[(t + KLA) % (KLA + 1)]);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-          sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[t % (KLA + 1)][kb], qf[t], sacc[kb], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      union VFrag {
-        s16x4 s[2];
-        f16x8 h;
-      };
-      VFrag vf[2][DB];
-      auto vread = [&](int g16, VFrag (&dst)[DB]) {
-        const int k1 = 16 * g16 + tr_key, k2 = k1 + 8;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const int col = 32 * d + tr_col;
-          dst[d].s[0] = lds_read_tr16((const bf16*)(vb + k1 * D + kv_chunk<D>(col >> 3, k1) * 8 + (col & 7)));
-          dst[d].s[1] = lds_read_tr16((const bf16*)(vb + k2 * D + kv_chunk<D>(col >> 3, k2) * 8 + (col & 7)));
-        }
-      };
-      vread(0, vf[0]);
-      // scores in log2 units: kf s + ve
-      float kfac[2], ve[2], vinv[2];
+    const float ks_after[2] = {ks_next[0], ks_next[1]}, vs_after[2] = {vs_next[0], vs_next[1]};
+    constexpr int KLA = 3;
+    f32x16 sacc[2] = {f32x16{0.f}, f32x16{0.f}};
+    f16x8 kf[KLA + 1][2];
+    auto kread = [&](int t, f16x8 (&dst)[2]) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const float f = ks[kb] * score_scale;
-        kfac[kb] = f < 1.17549435e-38f ? 1.17549435e-38f : f;  // (not 0: -inf * 0)
-        ve[kb] = scale_log2(vs[kb]);
-        vinv[kb] = scale_inverse(vs[kb]);
+        const int key = kb * 32 + lr;
+        dst[kb] = *(const f16x8*)&kb_lds[key * D + kv_chunk<D>(2 * t + lg, key) * 8];
       }
-      if (key0 + kKeys8 - 1 > wave_lo) {  // the causal edge crosses this tile
+    };
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+    for (int t = 0; t < KLA && t < DS; ++t) kread(t, kf[t]);
+    // (past the last tile the codes of the one before are converted again, for nobody)
+    each<DS>([&](auto t_) {
+      constexpr int t = decltype(t_)::value;
+      if constexpr (t + KLA < DS) kread(t + KLA, kf[(t + KLA) % (KLA + 1)]);
+      sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[t % (KLA + 1)][0], qf[t], sacc[0], 0, 0, 0);
+      convert(t_, other);
+      sacc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[t % (KLA + 1)][1], qf[t], sacc[1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    gload(kt + 2);
+    union VFrag {
+      s16x4 s[2];
+      f16x8 h;
+    };
+    VFrag vf[2][DB];
+    auto vread = [&](int g16, VFrag (&dst)[DB]) {
+      const int k1 = 16 * g16 + tr_key, k2 = k1 + 8;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int key = key0 + 32 * kb + (e & 3) + 8 * (e >> 2) + 4 * lg;
-            if (key > qpos) sacc[kb][e] = -INFINITY;
-          }
-          // a block past this row: none of its scales either (one may be NaN)
-          const bool none = key0 + 32 * kb > qpos;
-          kfac[kb] = none ? 1.f : kfac[kb];
-          ve[kb] = none ? 0.f : ve[kb];
-          vinv[kb] = none ? 1.f : vinv[kb];
-        }
+      for (int d = 0; d < DB; ++d) {
+        const int col = 32 * d + tr_col;
+        dst[d].s[0] = lds_read_tr16((const bf16*)(vb + k1 * D + kv_chunk<D>(col >> 3, k1) * 8 + (col & 7)));
+        dst[d].s[1] = lds_read_tr16((const bf16*)(vb + k2 * D + kv_chunk<D>(col >> 3, k2) * 8 + (col & 7)));
       }
-      const float thr = m_run + kSoftmaxSlack;
-      const float mh = fmaxf(fmaf(tree_max16(sacc[0]), kfac[0], ve[0]), fmaf(tree_max16(sacc[1]), kfac[1], ve[1]));
-      if (__builtin_amdgcn_ballot_w64(mh > thr)) {
-        const float mt = fmaxf(mh, __shfl_xor(mh, 32, 64));
-        const bool raise = mt > thr;
-        const float m_new = raise ? mt : m_run;
-        const float alpha = raise ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
-        m_run = m_new;
-        l_run *= alpha;
+    };
+    vread(0, vf[0]);
+    // scores in log2 units: kf s + ve
+    float kfac[2], ve[2], vinv[2];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) oacc[d] *= alpha;
-      }
-      // (a row that precedes every key so far has no maximum; its weights are 0)
-      const float m_use = m_run == -INFINITY ? 0.f : m_run;
-      f16x8 p[4];
+    for (int kb = 0; kb < 2; ++kb) {
+      const float f = ks[kb] * score_scale;
+      kfac[kb] = f < 1.17549435e-38f ? 1.17549435e-38f : f;  // (not 0: -inf * 0)
+      ve[kb] = scale_log2(vs[kb]);
+      vinv[kb] = scale_inverse(vs[kb]);
+    }
+    if (key0 + kKeys8 - 1 > wave_lo) {  // the causal edge crosses this tile
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const float off = ve[kb] - m_use;
-        float ls[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          float w[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(sacc[kb][8 * u + e], kfac[kb], off));
-          ls[u] = tree_sum8(w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[2 * kb + u][e] = (f16)w[e];
+        for (int e = 0; e < 16; ++e) {
+          const int key = key0 + 32 * kb + (e & 3) + 8 * (e >> 2) + 4 * lg;
+          if (key > qpos) sacc[kb][e] = -INFINITY;
         }
-        l_run = fmaf(ls[0] + ls[1], vinv[kb], l_run);
-      }
-#pragma unroll
-      for (int g16 = 0; g16 < 4; ++g16) {
-        if (g16 + 1 < 4) vread(g16 + 1, vf[(g16 + 1) & 1]);
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-          oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[g16 & 1][d].h, p[g16], oacc[d], 0, 0, 0);
+        // a block past this row: none of its scales either (one may be NaN)
+        const bool none = key0 + 32 * kb > qpos;
+        kfac[kb] = none ? 1.f : kfac[kb];
+        ve[kb] = none ? 0.f : ve[kb];
+        vinv[kb] = none ? 1.f : vinv[kb];
       }
     }
+    const float thr = m_run + kSoftmaxSlack;
+    const float mh = fmaxf(fmaf(tree_max16(sacc[0]), kfac[0], ve[0]), fmaf(tree_max16(sacc[1]), kfac[1], ve[1]));
+    if (__builtin_amdgcn_ballot_w64(mh > thr)) {
+      const float mt = fmaxf(mh, __shfl_xor(mh, 32, 64));
+      const bool raise = mt > thr;
+      const float m_new = raise ? mt : m_run;
+      const float alpha = raise ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) oacc[d] *= alpha;
+    }
+    // (a row that precedes every key so far has no maximum; its weights are 0)
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    const float off[2] = {ve[0] - m_use, ve[1] - m_use};
+    f16x8 p[2];          // weights of the 16 keys at work and of the next 16
+    float ls[4][2] = {};  // their sums, in pairs
+    auto weights = [&](auto g_, auto pair_) {
+      constexpr int g = decltype(g_)::value, i = decltype(pair_)::value, kb = g >> 1, e = 8 * (g & 1) + 2 * i;
+      const float a = __builtin_amdgcn_exp2f(fmaf(sacc[kb][e], kfac[kb], off[kb]));
+      const float c2 = __builtin_amdgcn_exp2f(fmaf(sacc[kb][e + 1], kfac[kb], off[kb]));
+      ls[g][0] = i == 0 ? a : ls[g][0] + a;
+      ls[g][1] = i == 0 ? c2 : ls[g][1] + c2;
+      p[g & 1][2 * i] = (f16)a;
+      p[g & 1][2 * i + 1] = (f16)c2;
+    };
+    each<4>([&](auto i) { weights(Int<0>{}, i); });
+    each<4>([&](auto g_) {
+      constexpr int g = decltype(g_)::value;
+      if constexpr (g + 1 < 4) vread(g + 1, vf[(g + 1) & 1]);
+      each<DB>([&](auto d_) {
+        constexpr int d = decltype(d_)::value;
+        oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[g & 1][d].h, p[g & 1], oacc[d], 0, 0, 0);
+        if constexpr (g + 1 < 4)
+          each<4 / DB>([&](auto j) { weights(Int<g + 1>{}, Int<d * (4 / DB) + decltype(j)::value>{}); });
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    l_run = fmaf((ls[0][0] + ls[0][1]) + (ls[1][0] + ls[1][1]), vinv[0], l_run);
+    l_run = fmaf((ls[2][0] + ls[2][1]) + (ls[3][0] + ls[3][1]), vinv[1], l_run);
     ks[0] = ks_after[0], ks[1] = ks_after[1], vs[0] = vs_after[0], vs[1] = vs_after[1];
   };
   for (int kt = kt_lo; kt < kt_hi; kt += 2) {
@@ -474,7 +478,7 @@ static int kv8_key_splits(const BatchDev& b, int n_q_heads, int n_kv_heads) {
   const int64_t wgs = (int64_t)cdiv(b.n_tokens * (n_q_heads / n_kv_heads), kRows8) * n_kv_heads;
   const int tiles = cdiv(b.max_ctx_len + b.max_q_len, kKeys8);
   int sp = 1;
-  while (sp < kMaxSplitF8 && wgs * sp * 2 * 4 <= (int64_t)cu_count() * 5 && tiles >= 16 * sp) sp *= 2;
+  while (sp < kMaxSplitF8 && wgs * sp * 2 <= (int64_t)cu_count() * 2 && tiles >= 16 * sp) sp *= 2;
   return sp;
 }
 
@@ -489,7 +493,7 @@ static size_t lse_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads) {
 static size_t part8_bytes(const BatchDev& b, int n_q_heads, int n_kv_heads, int head_dim) {
   if (b.max_q_len < 2) return 0;
   const int64_t rows = std::min<int64_t>((int64_t)kMaxSplitF8 * b.n_tokens * n_q_heads,
-                                         (int64_t)cu_count() * 5 / 4 * kRows8);
+                                         (int64_t)cu_count() * 2 * kRows8);
   return round256((size_t)rows * (head_dim + 4) * 4);
 }
 size_t attn_kv8_workspace_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads, int n_kv_heads,

@@ -305,39 +305,49 @@ __global__ __launch_bounds__(256) void attn_kv8_merge_kernel(
   if (!kv8_seq(b, c, s, t, n, ctx, sl) || n != 1) return;
   const int rows_seen = min(ctx, b.max_ctx_len) + 1;
   const int ns = min(cdiv(rows_seen, split_rows), nsplit);
-  const int lane = tid & 63, wave = tid >> 6;
   if ((int)blockIdx.x < mass_wgs) {
     const int grp = Hq / Hkv, chunks = mass_wgs / Hkv;
     const int h = (int)blockIdx.x / chunks, row0 = ((int)blockIdx.x % chunks) * kMassRows;
     if (row0 >= rows_seen) return;
-    for (int q = wave; q < grp; q += 4) {
-      const float* pp = part + ((int64_t)s * Hq + h * grp + q) * nsplit * (D + 4) + D;
+    // this thread's rows: their mass and the first heads' scores are under way while the
+    // heads' log-sum-exps are formed, eight threads a head
+    const int row = row0 + 4 * tid;
+    int prow = 0;
+    const int panel = row < rows_seen ? kv_panel(c.kv, sl, row, prow) : -1;
+    const float* sp = scores + ((int64_t)s * Hq + h * grp) * score_ld + (panel < 0 ? row0 : row);
+    float* mp = c.mass + kv8_row_at(c, Hkv, max(panel, 0), h, prow);
+    float before[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) before[e] = panel >= 0 && row + e < rows_seen ? mp[e] : 0.f;
+    f32x4 x[4];
+    auto load = [&](int q0) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = *(const f32x4*)(sp + (int64_t)min(q0 + q, grp - 1) * score_ld);
+    };
+    load(0);
+    {
+      const int q = tid >> 3;
+      const float* pp = part + ((int64_t)s * Hq + h * grp + min(q, grp - 1)) * nsplit * (D + 4) + D;
       float M = -INFINITY, L = 0.f;
-      for (int j = lane; j < ns; j += 64) {
+      for (int j = tid & 7; j < ns; j += 8) {
         const f32x2 ml = *(const f32x2*)(pp + (int64_t)j * (D + 4));
         const float Mn = fmaxf(M, ml[0]);
         L = (M == -INFINITY ? 0.f : L * exp2f(M - Mn)) + ml[1] * exp2f(ml[0] - Mn);
         M = Mn;
       }
-      const float top = wave_max(M);
-      L = wave_sum(lane < ns ? L * exp2f(M - top) : 0.f);
-      if (lane == 0) lse[q] = top + log2f(L);
+      float top = M;
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+      L = (tid & 7) < ns ? L * exp2f(M - top) : 0.f;
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) L += __shfl_xor(L, o, 64);
+      if ((tid & 7) == 0) lse[q] = top + log2f(L);
     }
     __syncthreads();
-    const int row = row0 + 4 * tid;
-    int prow = 0;
-    const int panel = row < rows_seen ? kv_panel(c.kv, sl, row, prow) : -1;
     if (panel < 0) return;
-    const float* sp = scores + ((int64_t)s * Hq + h * grp) * score_ld + row;
-    float* mp = c.mass + kv8_row_at(c, Hkv, panel, h, prow);
-    float before[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) before[e] = row + e < rows_seen ? mp[e] : 0.f;
     f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int q0 = 0; q0 < grp; q0 += 4) {
-      f32x4 x[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) x[q] = *(const f32x4*)(sp + (int64_t)min(q0 + q, grp - 1) * score_ld);
+      if (q0 > 0) load(q0);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if (q0 + q >= grp) break;

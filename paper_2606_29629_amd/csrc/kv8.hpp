@@ -9,6 +9,14 @@ template <int N>
 struct Int {
   static constexpr int value = N;
 };
+// f(Int<0>{}) ... f(Int<N - 1>{})
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (I < N) {
+    f(Int<I>{});
+    each<N, I + 1>(f);
+  }
+}
 
 constexpr int kKv8LeastExp = -100;  // exponent of the smallest scale
 
