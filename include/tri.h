@@ -392,6 +392,24 @@ tri_status tri_kv8_attention(const tri_layer_config* cfg, const tri_kv8_cache* c
                              const tri_batch* batch, const void* q, int64_t q_stride, void* out,
                              void* workspace, size_t workspace_bytes, void* stream);
 
+/* The decoder layer over an 8-bit cache: tri_layer_prefill and tri_layer_decode with the
+ * cache written by tri_kv8_append and attended to by tri_kv8_attention (mass included)
+ * in place of the bf16 cache; every other stage is the same.  cfg->dtype is TRI_BF16.
+ * The attention sees the step's own rows as the cache holds them.  workspace: of
+ * tri_workspace_size_kv8 bytes.                                                   */
+tri_status tri_workspace_size_kv8(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                                  const tri_batch* batch, size_t* bytes);
+tri_status tri_layer_prefill_kv8(const tri_layer_config* cfg, const tri_layer_weights* w,
+                                 const tri_kv8_cache* cache, const tri_batch* batch,
+                                 const void* x_in, void* x_out, int32_t* route_idx,
+                                 float* route_w, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+tri_status tri_layer_decode_kv8(const tri_layer_config* cfg, const tri_layer_weights* w,
+                                const tri_kv8_cache* cache, const tri_batch* batch,
+                                const void* x_in, void* x_out, int32_t* route_idx,
+                                float* route_w, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
 /* Eviction, first half: which rows stay.  Of the n = ctx_len[s] + q_len rows of a
  * sequence's slot, every KV head keeps `budget` (all where n <= budget): rows with
  * stamp < n_first or stamp > newest - n_recent (newest: the largest stamp of the

@@ -123,6 +123,11 @@ _FUNCS = {
     "tri_rope": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                 ctypes.c_int64, ctypes.c_void_p] + [ctypes.c_int32] * 3
                  + [ctypes.c_void_p]),
+    "tri_workspace_size_kv8": (ctypes.c_int, [ctypes.c_void_p] * 4),
+    "tri_layer_prefill_kv8": (ctypes.c_int, [ctypes.c_void_p] * 9
+                              + [ctypes.c_size_t, ctypes.c_void_p]),
+    "tri_layer_decode_kv8": (ctypes.c_int, [ctypes.c_void_p] * 9
+                             + [ctypes.c_size_t, ctypes.c_void_p]),
     "tri_kv8_append": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int64, ctypes.c_void_p]),
     "tri_kv8_attention_workspace_size": (ctypes.c_int, [ctypes.c_void_p] * 4),
     "tri_kv8_attention": (ctypes.c_int, [ctypes.c_void_p] * 4
@@ -241,9 +246,14 @@ def weights_struct(w: Dict[str, object]) -> LayerWeights:
                            "w_down", "w_router", "q_norm", "k_norm")])
 
 
-def workspace_size(cfg: LayerConfig, batch: DeviceBatch) -> int:
+def workspace_size(cfg: LayerConfig, batch: DeviceBatch, cache=None) -> int:
+    """Workspace bytes of a layer call; cache: the KV8Cache of one on an 8-bit cache."""
     n = ctypes.c_size_t(0)
     b = batch.struct()
+    if isinstance(cache, KV8Cache):
+        _check(lib().tri_workspace_size_kv8(ctypes.byref(cfg), cache._ref, ctypes.byref(b),
+                                            ctypes.byref(n)), "tri_workspace_size_kv8")
+        return n.value
     _check(lib().tri_workspace_size(ctypes.byref(cfg), ctypes.byref(b), ctypes.byref(n)),
            "tri_workspace_size")
     return n.value
@@ -285,11 +295,16 @@ def _layer(fn_name, cfg, w, cache, batch, x, out, workspace, route_idx, route_w,
     import torch
     if out is None:
         out = torch.empty_like(x)
-    need = workspace_size(cfg, batch)
+    if isinstance(cache, KV8Cache):
+        if (cfg.n_kv_heads, cfg.head_dim) != (cache.n_kv_heads, cache.head_dim):
+            raise ValueError(f"{fn_name}: the cache has {cache.n_kv_heads} heads of {cache.head_dim}")
+        fn_name, kc = fn_name + "_kv8", cache.struct()
+    else:
+        kc = kv_struct(cache)
+    need = workspace_size(cfg, batch, cache)
     if workspace is None:
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=x.device)
     ws = weights_struct(w)
-    kc = kv_struct(cache)
     b = batch.struct()
     st = getattr(lib(), fn_name)(ctypes.byref(cfg), ctypes.byref(ws), ctypes.byref(kc),
                                  ctypes.byref(b), _ptr(x), _ptr(out), _ptr(route_idx),
@@ -301,14 +316,16 @@ def _layer(fn_name, cfg, w, cache, batch, x, out, workspace, route_idx, route_w,
 
 def layer_prefill(cfg, w, cache, batch, x, out=None, workspace=None, route_idx=None,
                   route_w=None, stream=None):
-    """One decoder layer over a ragged batch; returns (out, workspace)."""
+    """One decoder layer over a ragged batch; returns (out, workspace).  cache: a (k, v)
+    pair, a PagedCache or a KV8Cache."""
     return _layer("tri_layer_prefill", cfg, w, cache, batch, x, out, workspace, route_idx,
                   route_w, stream)
 
 
 def layer_decode(cfg, w, cache, batch, x, out=None, workspace=None, route_idx=None,
                  route_w=None, stream=None):
-    """One decode step (one new token per sequence); returns (out, workspace)."""
+    """One decode step (one new token per sequence); returns (out, workspace).  cache: as in
+    layer_prefill."""
     return _layer("tri_layer_decode", cfg, w, cache, batch, x, out, workspace, route_idx,
                   route_w, stream)
 

@@ -68,6 +68,8 @@ tri_status tri::check_batch_scalars(const tri_batch* b) {
 
 namespace {
 
+constexpr int kMaxGridYZ = 65535;  // sequences and heads over an 8-bit cache
+
 // Projections with at most this many rows take the weight-streaming path.
 constexpr int kSkinnyMaxRows = 128;
 
@@ -78,6 +80,8 @@ struct Layout {
   // fp32 storage: bf16 operand planes of the activations (one GEMM at a time)
   // and of the weights (q/k/v, O, gate/up, down)
   size_t a3, w_qkv3, w_o3, w_gu3, w_d3;
+  // 8-bit cache: the new keys and values, the attention's workspace
+  size_t k_new, v_new, kv8;
   size_t total;
 };
 
@@ -189,7 +193,13 @@ Layout layout_f32(const tri_layer_config* c, const tri_batch* b) {
   return l;
 }
 
-Layout layout_of(const tri_layer_config* c, const tri_batch* b) {
+BatchDev batch_dev(const tri_batch* b) {
+  return BatchDev{b->cu_q, b->ctx_len, b->slot, b->pos, b->n_seqs, b->n_tokens, b->max_q_len,
+                  b->max_ctx_len};
+}
+
+Layout layout_of(const tri_layer_config* c, const tri_batch* b,
+                 const tri_kv8_cache* cache8 = nullptr) {
   if (is_f32(c)) return layout_f32(c, b);
   const size_t T = (size_t)b->n_tokens, H = c->hidden, D = c->head_dim;
   const bool moe = is_moe(c);
@@ -222,6 +232,14 @@ Layout layout_of(const tri_layer_config* c, const tri_batch* b) {
   // bound that never decreases with T.
   const size_t rows = moe ? std::max(T, (size_t)51200 / ((E + 63) / 64)) : 0;
   l.logits = o;   o += up(rows * plane_ld((int)E) * 4);
+  if (cache8) {
+    l.k_new = o;  o += up(T * c->n_kv_heads * D * 2);
+    l.v_new = o;  o += up(T * c->n_kv_heads * D * 2);
+    l.kv8 = o;
+    if (T > 0)
+      o += up(attn_kv8_workspace_bytes(batch_dev(b), kv8_dev(cache8), c->n_q_heads, c->n_kv_heads,
+                                       c->head_dim));
+  }
   l.total = o;
   return l;
 }
@@ -407,15 +425,17 @@ tri_status layer_f32(const tri_layer_config* cfg, const tri_layer_weights* w,
 tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
                            const tri_layer_weights* w, const tri_kv_cache* cache,
                            const tri_batch* b, const void* x_in, void* x_out, int32_t* route_idx,
-                           float* route_w, void* ws, size_t ws_bytes, void* stream) {
+                           float* route_w, void* ws, size_t ws_bytes, void* stream,
+                           const tri_kv8_cache* cache8) {
   tri_status st = check_config(cfg);
   if (st != TRI_OK) return st;
-  if (!w || !cache) return TRI_ERR_NULL;
+  if (!w || (!cache && !cache8)) return TRI_ERR_NULL;
+  if (cache8 && is_f32(cfg)) return TRI_ERR_UNSUPPORTED;
   if ((st = check_batch_scalars(b)) != TRI_OK) return st;
   if (decode && (b->n_tokens != b->n_seqs || b->max_q_len > 1)) return TRI_ERR_SHAPE;
   if (b->n_tokens == 0) return TRI_OK;
   if (!x_in || !x_out || !ws || !b->cu_q || !b->ctx_len || !b->slot || !b->pos) return TRI_ERR_NULL;
-  if ((st = check_cache(cache)) != TRI_OK) return st;
+  if ((st = cache8 ? check_kv8_cache(cache8) : check_cache(cache)) != TRI_OK) return st;
   if (!w->attn_norm || !w->w_qkv || !w->w_o || !w->mlp_norm || !w->w_gate_up || !w->w_down)
     return TRI_ERR_NULL;
   const bool moe = is_moe(cfg);
@@ -424,9 +444,12 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
   if (bias && !w->b_qkv) return TRI_ERR_NULL;
   const bool qk_norm = (cfg->flags & TRI_F_QK_NORM) != 0;
   if (qk_norm && (!w->q_norm || !w->k_norm)) return TRI_ERR_NULL;
-  if (b->max_ctx_len >= cache->max_seq || b->max_q_len > cache->max_seq) return TRI_ERR_RANGE;
-  if (decode && (int64_t)b->max_ctx_len + 1 > cache->max_seq) return TRI_ERR_RANGE;
-  const void* ptrs[] = {x_in, x_out, ws, cache->k, cache->v, w->attn_norm, w->w_qkv, w->w_o,
+  const int max_seq = cache8 ? cache8->max_seq : cache->max_seq;
+  if (b->max_ctx_len >= max_seq || b->max_q_len > max_seq) return TRI_ERR_RANGE;
+  if (decode && (int64_t)b->max_ctx_len + 1 > max_seq) return TRI_ERR_RANGE;
+  if (cache8 && (b->n_seqs > kMaxGridYZ || cfg->n_q_heads > kMaxGridYZ)) return TRI_ERR_RANGE;
+  const void* ptrs[] = {x_in, x_out, ws, cache8 ? cache8->k : cache->k,
+                        cache8 ? cache8->v : cache->v, w->attn_norm, w->w_qkv, w->w_o,
                         w->mlp_norm, w->w_gate_up, w->w_down};
   for (const void* p : ptrs)
     if (!aligned16(p)) return TRI_ERR_ALIGN;
@@ -434,7 +457,7 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
   if (qk_norm && (!aligned16(w->q_norm) || !aligned16(w->k_norm))) return TRI_ERR_ALIGN;
   if (moe && !aligned16(w->w_router)) return TRI_ERR_ALIGN;
   if (((uintptr_t)ws & (kAlign - 1)) != 0) return TRI_ERR_ALIGN;
-  const Layout L = layout_of(cfg, b);
+  const Layout L = layout_of(cfg, b, cache8);
   if (ws_bytes < L.total) return TRI_ERR_WORKSPACE;
   const size_t act_bytes = (size_t)b->n_tokens * cfg->hidden * (is_f32(cfg) ? 4 : 2);
   if (overlaps(x_in, act_bytes, x_out, act_bytes)) return TRI_ERR_ALIAS;
@@ -448,9 +471,9 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
   const int T = b->n_tokens, H = cfg->hidden, D = cfg->head_dim;
   const int Hq = cfg->n_q_heads, Hkv = cfg->n_kv_heads, F = cfg->ffn_dim;
   const int Nqkv = (Hq + 2 * Hkv) * D;
-  BatchDev bd{b->cu_q, b->ctx_len, b->slot, b->pos, b->n_seqs, b->n_tokens, b->max_q_len,
-              b->max_ctx_len};
-  const KvDev kv = kv_dev(cache);
+  const BatchDev bd = batch_dev(b);
+  // (8-bit cache: the new rows go to the workspace, [T][Hkv][D], and are appended from there)
+  const KvDev kv = cache8 ? KvDev{} : kv_dev(cache);
   int32_t* tok_slot = at<int32_t>(ws, L.tok_slot);
   int32_t* tok_row = at<int32_t>(ws, L.tok_row);
   float2* rope = at<float2>(ws, L.rope);
@@ -472,8 +495,8 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
   e.kind = EPI_QKV;
   e.bias = bias ? w->b_qkv : nullptr;
   e.q = q;
-  e.kc = cache->k;
-  e.vc = cache->v;
+  e.kc = cache8 ? at<void>(ws, L.k_new) : cache->k;
+  e.vc = cache8 ? at<void>(ws, L.v_new) : cache->v;
   e.tok_slot = tok_slot;
   e.tok_row = tok_row;
   e.rope = rope;
@@ -483,37 +506,48 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
   e.n_q_heads = Hq;
   e.n_kv_heads = Hkv;
   e.head_dim = D;
-  e.max_seq = kv.panel_rows();
+  e.max_seq = cache8 ? 1 : kv.panel_rows();
   e.routed = moe;
   {
     StageTimer t_(ST_QKV, s, timed);
     if ((st = run_linear(h, H, w->w_qkv, T, Nqkv, H, e, part, s)) != TRI_OK) return st;
   }
-  // Flash attention serves the multi-token sequences, split-KV attention the
-  // single-token ones (a batch in which every sequence has max_q_len > 1
-  // tokens has none).  When a batch has both, the split-KV kernels run on the
-  // side stream, overlapping the compute-bound flash kernel with the
-  // memory-bound decode attention.
-  const bool flash = !decode && b->max_q_len > 1;
-  const bool splitkv =
-      decode || b->max_q_len == 1 || (int64_t)b->n_seqs * b->max_q_len != b->n_tokens;
-  float* part_dec = (float*)((char*)part + flash_part_bytes(cfg, b));
-  Fork fork;
-  if (flash && splitkv) TRI_HIP(fork.begin(s));
-  hipStream_t sd = fork.stream ? fork.stream : s;  // stream of the split-KV attention
-  if (splitkv) {
+  if (cache8) {
+    const Kv8Dev c8 = kv8_dev(cache8);
+    const bool fp8 = cache8->format == TRI_KV8_E4M3;
     {
-      StageTimer t_(ST_ATTN_DECODE, sd, timed);
-      TRI_HIP(launch_attn_decode_split(q, cache->k, cache->v, part_dec, bd, kv, Hq, Hkv, D, sd));
+      StageTimer t_(ST_APPEND, s, timed);
+      TRI_HIP(launch_kv8_append(bd, c8, fp8, Hkv, D, e.kc, e.vc, (int64_t)Hkv * D, s));
     }
-    StageTimer t_(ST_ATTN_COMBINE, sd, timed);
-    TRI_HIP(launch_attn_decode_combine(part_dec, attn, bd, kv, Hq, Hkv, D, sd));
+    StageTimer t_(decode ? ST_ATTN_DECODE : ST_ATTN_PREFILL, s, timed);
+    TRI_HIP(launch_attn_kv8(bd, c8, fp8, Hq, Hkv, D, q, (int64_t)Hq * D, attn, at<void>(ws, L.kv8), s));
+  } else {
+    // Flash attention serves the multi-token sequences, split-KV attention the
+    // single-token ones (a batch in which every sequence has max_q_len > 1
+    // tokens has none).  When a batch has both, the split-KV kernels run on the
+    // side stream, overlapping the compute-bound flash kernel with the
+    // memory-bound decode attention.
+    const bool flash = !decode && b->max_q_len > 1;
+    const bool splitkv =
+        decode || b->max_q_len == 1 || (int64_t)b->n_seqs * b->max_q_len != b->n_tokens;
+    float* part_dec = (float*)((char*)part + flash_part_bytes(cfg, b));
+    Fork fork;
+    if (flash && splitkv) TRI_HIP(fork.begin(s));
+    hipStream_t sd = fork.stream ? fork.stream : s;  // stream of the split-KV attention
+    if (splitkv) {
+      {
+        StageTimer t_(ST_ATTN_DECODE, sd, timed);
+        TRI_HIP(launch_attn_decode_split(q, cache->k, cache->v, part_dec, bd, kv, Hq, Hkv, D, sd));
+      }
+      StageTimer t_(ST_ATTN_COMBINE, sd, timed);
+      TRI_HIP(launch_attn_decode_combine(part_dec, attn, bd, kv, Hq, Hkv, D, sd));
+    }
+    if (flash) {
+      StageTimer t_(ST_ATTN_PREFILL, s, timed);
+      TRI_HIP(launch_attn_prefill(q, cache->k, cache->v, attn, bd, kv, Hq, Hkv, D, 0, part, s));
+    }
+    TRI_HIP(fork.end());
   }
-  if (flash) {
-    StageTimer t_(ST_ATTN_PREFILL, s, timed);
-    TRI_HIP(launch_attn_prefill(q, cache->k, cache->v, attn, bd, kv, Hq, Hkv, D, 0, part, s));
-  }
-  TRI_HIP(fork.end());
   e = Epi{};
   e.kind = EPI_RESID;
   e.out = x1;
@@ -664,6 +698,34 @@ tri_status tri_layer_decode(const tri_layer_config* cfg, const tri_layer_weights
                             size_t workspace_bytes, void* stream) {
   return layer_call(true, true, cfg, w, cache, batch, x_in, x_out, route_idx, route_w,
                     workspace, workspace_bytes, stream);
+}
+
+tri_status tri_workspace_size_kv8(const tri_layer_config* cfg, const tri_kv8_cache* cache,
+                                  const tri_batch* batch, size_t* bytes) {
+  if (!bytes) return TRI_ERR_NULL;
+  tri_status st = check_config(cfg);
+  if (st != TRI_OK) return st;
+  if (is_f32(cfg)) return TRI_ERR_UNSUPPORTED;
+  if ((st = check_kv8_cache(cache)) != TRI_OK) return st;
+  if ((st = check_batch_scalars(batch)) != TRI_OK) return st;
+  *bytes = layout_of(cfg, batch, cache).total;
+  return TRI_OK;
+}
+
+tri_status tri_layer_prefill_kv8(const tri_layer_config* cfg, const tri_layer_weights* w,
+                                 const tri_kv8_cache* cache, const tri_batch* batch,
+                                 const void* x_in, void* x_out, int32_t* route_idx, float* route_w,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  return layer_call(false, true, cfg, w, nullptr, batch, x_in, x_out, route_idx, route_w,
+                    workspace, workspace_bytes, stream, cache);
+}
+
+tri_status tri_layer_decode_kv8(const tri_layer_config* cfg, const tri_layer_weights* w,
+                                const tri_kv8_cache* cache, const tri_batch* batch,
+                                const void* x_in, void* x_out, int32_t* route_idx, float* route_w,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  return layer_call(true, true, cfg, w, nullptr, batch, x_in, x_out, route_idx, route_w,
+                    workspace, workspace_bytes, stream, cache);
 }
 
 tri_status tri_kvcache_append(const tri_layer_config* cfg, const tri_kv_cache* cache,

@@ -24,7 +24,7 @@ namespace tri {
 
 constexpr int kRows8 = 128;    // packed query rows per workgroup
 constexpr int kKeys8 = 64;     // cache rows per tile
-constexpr int kMaxSplitF8 = 8;  // key-range splits of a row tile, at most
+constexpr int kMaxSplitF8 = 32;  // key-range splits of a row tile, at most
 
 // Thread i of 256 (and 256 more for D = 128) moves 16 codes of a tile: row and chunk, rows
 // ordered so that 16 neighbouring threads' float16 chunks fall on different banks (the
@@ -323,24 +323,26 @@ __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c
     const int nkt = cdiv(ctx + last / G + 1, kKeys8), ns = cdiv(nkt, cdiv(nkt, nsplit));
     const int64_t at = (int64_t)h * b.n_tokens * G + (int64_t)q0 * G + row;
     const float* pp = part + at * (D + 4);
-    f32x2 ml[kMaxSplitF8];
-    f32x4 a[kMaxSplitF8];
-#pragma unroll
-    for (int j = 0; j < kMaxSplitF8; ++j) {  // (splits past the last are loaded again and dropped)
-      const float* pj = pp + min(j, ns - 1) * plane;
-      ml[j] = *(const f32x2*)(pj + D);
-      a[j] = *(const f32x4*)(pj + d);
-    }
     float M = -INFINITY, L = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j0 = 0; j0 < ns; j0 += 8) {
+      f32x2 ml[8];
+      f32x4 a[8];
 #pragma unroll
-    for (int j = 0; j < kMaxSplitF8; ++j) {
-      if (j >= ns || (ml[j][0] == -INFINITY && ml[j][1] == 0.f)) continue;  // no key of it visible
-      const float Mn = fmaxf(M, ml[j][0]);
-      const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[j][0] - Mn);
-      L = L * x + ml[j][1] * w;
-      o = o * x + a[j] * w;
-      M = Mn;
+      for (int j = 0; j < 8; ++j) {  // (splits past the last are loaded again and dropped)
+        const float* pj = pp + min(j0 + j, ns - 1) * plane;
+        ml[j] = *(const f32x2*)(pj + D);
+        a[j] = *(const f32x4*)(pj + d);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j0 + j >= ns || (ml[j][0] == -INFINITY && ml[j][1] == 0.f)) continue;  // no key visible
+        const float Mn = fmaxf(M, ml[j][0]);
+        const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[j][0] - Mn);
+        L = L * x + ml[j][1] * w;
+        o = o * x + a[j] * w;
+        M = Mn;
+      }
     }
     bf16x4 o4;
 #pragma unroll
@@ -351,22 +353,25 @@ __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c
 }
 
 // mass[key] += sum over the packed rows of 2^(score - lse): the scores once more, keys and
-// rows the other way round.  One workgroup = 128 cache rows of a KV head, each of four wave
-// pairs 32 of them with their codes in registers as bf16 (exact too, and q needs no
-// conversion); query rows come 64 at a time through LDS by direct loads, 32 to each wave of
-// a pair, so that a SIMD's two waves cover each other's waits.  Every sum has one order.
-constexpr int kMassKeys = 128, kMassQ = 64;
-
-template <int D, bool FP8>
+// rows the other way round.  A workgroup of eight waves has KG groups of 32 cache rows, their
+// codes in registers as bf16 (exact too, and q needs no conversion); query rows come 32 RG =
+// 256 / KG at a time through LDS by direct loads, 32 to each of a group's RG waves, so that a
+// SIMD's two waves cover each other's waits.  Every sum has one order.  Fewer groups make
+// more workgroups of fewer steps that read the queries more often: KG = 4 where that fills
+// two thirds of the CUs, 2 down to a third, else 1 (whole calls with 4, 2 and 1: 4 chunks of
+// 300 to 900 tokens, 2 KV heads of 64, 66 workgroups at 4: 97, 73, 62 us; 200 tokens at 2000
+// beside single ones, 4 heads of 128, 144: 72, 65, 73; 8 x 1024, 256: 174, 186, 273).
+template <int D, bool FP8, int KG>
 __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
                                                                const bf16* __restrict__ Q, int64_t qs,
                                                                const float* __restrict__ lse,
                                                                float scale_log2e) {
   constexpr int DS = D / 16, DC = D / 8;
   constexpr int RPB = 64 / DC;             // rows of a 1 KB load
+  constexpr int RG = 8 / KG, kMassKeys = 32 * KG, kMassQ = 32 * RG;
   constexpr int NL = kMassQ / RPB / 8;     // such loads of a wave and tile
   __shared__ __align__(16) bf16 sq0[kMassQ * D], sq1[kMassQ * D];
-  __shared__ float upper[4][32];
+  __shared__ float sums[RG][KG][32];
   const int s = blockIdx.z, h = blockIdx.y, key0 = blockIdx.x * kMassKeys;
   int q0, n, ctx, sl;
   if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2 || key0 >= ctx + n) return;
@@ -375,7 +380,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lg = lane >> 5;
   // codes of this wave's 32 keys: lane key lr, values 16 t + 8 lg ...
-  const int half = wave >> 2, wkey = key0 + 32 * (wave & 3);
+  const int kg = wave % KG, rg = wave / KG, wkey = key0 + 32 * kg;
   int prow = 0;
   const int panel = wkey < ctx + n ? kv_panel(c.kv, sl, wkey, prow) : -1;
   const int live = panel < 0 ? 0 : min(32, ctx + n - wkey);
@@ -417,7 +422,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
   const float* lp = lse + (int64_t)h * b.n_tokens * G + (int64_t)q0 * G;
   auto lse_of = [&](int rt) {
-    const int row = rt * kMassQ + 32 * half + lr;
+    const int row = rt * kMassQ + 32 * rg + lr;
     return row < rows ? lp[row] : INFINITY;
   };
   float off_next = lse_of(rt_lo);
@@ -431,7 +436,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
       gload(rt + 1, Int<1 - decltype(buf)::value>{});
     }
     const bf16* qb = decltype(buf)::value ? sq1 : sq0;
-    const int r = 32 * half + lr, row = rt * kMassQ + r;
+    const int r = 32 * rg + lr, row = rt * kMassQ + r;
     const int qpos = ctx + min(row, rows - 1) / G;
     f32x16 sc = f32x16{0.f};
 #pragma unroll
@@ -454,33 +459,39 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
     step(rt, Int<0>{});
     if (rt + 1 < rt_hi) step(rt + 1, Int<1>{});
   }
-  // the pair's halves: the upper one's sums through LDS
+  // the group's waves: their sums through LDS, added in order
   float* mp = c.mass + kv8_row_at(c, Hkv, max(panel, 0), h, prow);
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = group_sum(acc[e], 32);
-  if (half == 1 && lr == 0) {
+  if (lr == 0) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) upper[wave & 3][(e & 3) + 8 * (e >> 2) + 4 * lg] = acc[e];
+    for (int e = 0; e < 16; ++e) sums[rg][kg][(e & 3) + 8 * (e >> 2) + 4 * lg] = acc[e];
   }
   __syncthreads();
-  if (half == 0 && lr == 0) {
+  if (rg == 0 && lane < live) {
+    float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int k = (e & 3) + 8 * (e >> 2) + 4 * lg;
-      if (k < live) mp[k] += acc[e] + upper[wave][k];
-    }
+    for (int r = 0; r < RG; ++r) sum += sums[r][kg][lane];
+    mp[lane] += sum;
   }
 }
 
-// Key-range splits: doubled while the workgroups still fit about one per CU and every
-// split keeps 8 tiles of the longest range.
+// Key-range splits: doubled while the workgroups fit one to a CU and a split keeps 4 tiles of
+// the longest range, or two to a CU and it keeps 8.  (512 tokens at 6144 beside 32 single
+// ones, 28/4 heads of 128, 112 workgroups unsplit: 190 us with two splits, 173 with four; 40
+// tokens at 6000, 12: 37 us with eight, 31 with sixteen; 500 at 1000 beside single ones, 14/2
+// heads of 64, 60: 31 us with four, 37 with eight.)
 static int kv8_key_splits(const BatchDev& b, int n_q_heads, int n_kv_heads) {
   const int64_t wgs = (int64_t)cdiv(b.n_tokens * (n_q_heads / n_kv_heads), kRows8) * n_kv_heads;
-  const int tiles = cdiv(b.max_ctx_len + b.max_q_len, kKeys8);
+  const int tiles = cdiv(b.max_ctx_len + b.max_q_len, kKeys8), cus = cu_count();
   int sp = 1;
-  while (sp < kMaxSplitF8 && wgs * sp * 2 <= (int64_t)cu_count() * 2 && tiles >= 16 * sp) sp *= 2;
+  while (sp < kMaxSplitF8 && ((wgs * sp * 2 <= cus && tiles >= 8 * sp) ||
+                              (wgs * sp * 2 <= 2 * cus && tiles >= 16 * sp)))
+    sp *= 2;
   return sp;
 }
+
+constexpr int64_t kForkBytes = (int64_t)192 << 20;  // codes that single tokens may read, for a side stream
 
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -526,9 +537,17 @@ static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (c.mass) {
-    attn_kv8_mass_kernel<D, FP8><<<dim3(cdiv(b.max_ctx_len + b.max_q_len, kMassKeys), Hkv, b.n_seqs), 512, 0, s>>>(
-        b, c, Hq, Hkv, (const bf16*)q, qs, lse, scale_log2e);
-    e = hipGetLastError();
+    // (as many chunks as the longest would make of the tokens)
+    const int64_t wgs4 = (int64_t)cdiv(b.max_ctx_len + b.max_q_len, 128) * Hkv * cdiv(b.n_tokens, b.max_q_len);
+    auto weigh = [&](auto kg, auto kernel) {
+      const int keys = 32 * decltype(kg)::value;
+      kernel<<<dim3(cdiv(b.max_ctx_len + b.max_q_len, keys), Hkv, b.n_seqs), 512, 0, s>>>(
+          b, c, Hq, Hkv, (const bf16*)q, qs, lse, scale_log2e);
+      return hipGetLastError();
+    };
+    if (wgs4 * 3 >= 2 * cu_count()) e = weigh(Int<4>{}, attn_kv8_mass_kernel<D, FP8, 4>);
+    else if (wgs4 * 3 >= cu_count()) e = weigh(Int<2>{}, attn_kv8_mass_kernel<D, FP8, 2>);
+    else e = weigh(Int<1>{}, attn_kv8_mass_kernel<D, FP8, 1>);
   }
   return e;
 }
@@ -543,12 +562,17 @@ hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q
     return launch_attn_kv8_decode(b, c, fp8, n_q_heads, n_kv_heads, head_dim, q, q_stride, out, own, st);
   };
   if (b.max_q_len == 1) return singles(s);
-  // Single tokens beside chunks: on the side stream (memory-bound beside compute-bound;
-  // other output rows, other weights' rows, another part of the workspace).
+  // Single tokens beside chunks, memory-bound beside compute-bound: on the side stream where
+  // their stream is long enough (other output rows, other weights' rows, another part of the
+  // workspace).  Fork and join cost about 20 us, so it pays from some 40 us of streaming:
+  // 33 sequences up to 8192 rows (277 MB at most) take 173 us so and 190 in turn, up
+  // to 4000 rows (135 MB) 87 us either way, 9 up to 600 45 and 28 us.
   Fork fork;
   hipError_t e = hipSuccess;
   if ((int64_t)b.n_seqs * b.max_q_len != b.n_tokens) {
-    if ((e = fork.begin(s)) == hipSuccess) e = singles(fork.stream);
+    const int64_t bytes = (int64_t)b.n_seqs * (b.max_ctx_len + 1) * n_kv_heads * head_dim * 2;
+    if (bytes >= kForkBytes) e = fork.begin(s);
+    if (e == hipSuccess) e = singles(fork.stream ? fork.stream : s);
   }
   if (e == hipSuccess) {
     if (head_dim == 128)

@@ -33,12 +33,16 @@ inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// The same for an 8-bit cache.
+tri_status check_kv8_cache(const tri_kv8_cache* c);
+
 // The layer entry points' common body (tri_layer_prefill when decode is
-// false, tri_layer_decode when true) on a workspace of ws_bytes; with timed =
+// false, tri_layer_decode when true) on a workspace of ws_bytes, over `cache` or, where it is
+// given, the 8-bit cache8; with timed =
 // false no profiling event is created or recorded.
 tri_status layer_call(bool decode, bool timed, const tri_layer_config* cfg,
                       const tri_layer_weights* w, const tri_kv_cache* cache, const tri_batch* b,
                       const void* x_in, void* x_out, int32_t* route_idx, float* route_w, void* ws,
-                      size_t ws_bytes, void* stream);
+                      size_t ws_bytes, void* stream, const tri_kv8_cache* cache8 = nullptr);
 
 }  // namespace tri

@@ -81,7 +81,7 @@ struct RopeSections {
 };
 
 // Layer prologue: per-token map (cache panel and row within it of every
-// token, -1 when out of range), the rotary table rope[t][i] = (cos, sin)(p *
+// token, -1 when out of range; with kv.max_seq 0 token t's panel is t, row 0), the rotary table rope[t][i] = (cos, sin)(p *
 // base^(-2i/D)) with p the token's position in frequency i's section (angle in
 // double precision), and y = RMSNorm(x) * g.
 // x, g, y are bf16, or fp32 with f32 (the fp32 storage mode), which also writes
@@ -213,6 +213,7 @@ struct Kv8Dev {
     return (kv.panel_rows() + (1 << scale_shift) - 1) >> scale_shift;
   }
 };
+Kv8Dev kv8_dev(const tri_kv8_cache* c);
 hipError_t launch_kv8_append(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_kv_heads,
                              int head_dim, const void* k_new, const void* v_new, int64_t stride,
                              hipStream_t s);

@@ -11,21 +11,7 @@
 
 using namespace tri;
 
-namespace {
-
-constexpr int kMaxGrid = 65535;  // y and z extents of a grid
-
-// The fields of the layer config that these operators read.
-tri_status check_heads(const tri_layer_config* c) {
-  if (!c) return TRI_ERR_NULL;
-  if (c->dtype != TRI_BF16) return TRI_ERR_UNSUPPORTED;
-  if (c->head_dim != 64 && c->head_dim != 128) return TRI_ERR_UNSUPPORTED;
-  if (c->n_kv_heads <= 0) return TRI_ERR_SHAPE;
-  if (c->n_kv_heads > kMaxGrid) return TRI_ERR_RANGE;
-  return TRI_OK;
-}
-
-tri_status check_cache8(const tri_kv8_cache* c) {
+tri_status tri::check_kv8_cache(const tri_kv8_cache* c) {
   if (!c) return TRI_ERR_NULL;
   if (!c->k || !c->v || !c->k_scale || !c->v_scale) return TRI_ERR_NULL;
   if (c->n_slots <= 0 || c->max_seq <= 0) return TRI_ERR_SHAPE;
@@ -43,7 +29,7 @@ tri_status check_cache8(const tri_kv8_cache* c) {
   return TRI_OK;
 }
 
-Kv8Dev kv8_dev(const tri_kv8_cache* c) {
+Kv8Dev tri::kv8_dev(const tri_kv8_cache* c) {
   Kv8Dev d{};
   d.kv = KvDev{c->n_slots, c->max_seq, c->block_table, c->block_table ? c->block_size : 0,
                c->block_table ? c->n_blocks : 0};
@@ -55,6 +41,20 @@ Kv8Dev kv8_dev(const tri_kv8_cache* c) {
   d.stamp = c->stamp;
   d.scale_shift = c->scale_rows == 32 ? 5 : (c->scale_rows == 64 ? 6 : 7);
   return d;
+}
+
+namespace {
+
+constexpr int kMaxGrid = 65535;  // y and z extents of a grid
+
+// The fields of the layer config that these operators read.
+tri_status check_heads(const tri_layer_config* c) {
+  if (!c) return TRI_ERR_NULL;
+  if (c->dtype != TRI_BF16) return TRI_ERR_UNSUPPORTED;
+  if (c->head_dim != 64 && c->head_dim != 128) return TRI_ERR_UNSUPPORTED;
+  if (c->n_kv_heads <= 0) return TRI_ERR_SHAPE;
+  if (c->n_kv_heads > kMaxGrid) return TRI_ERR_RANGE;
+  return TRI_OK;
 }
 
 BatchDev batch_dev(const tri_batch* b) {
@@ -69,7 +69,7 @@ tri_status check_call(const tri_layer_config* cfg, const tri_kv8_cache* cache, c
   if (!cache) return TRI_ERR_NULL;
   if ((st = check_batch_scalars(b)) != TRI_OK) return st;
   if (b->n_seqs == 0) return TRI_OK;
-  if ((st = check_cache8(cache)) != TRI_OK) return st;
+  if ((st = check_kv8_cache(cache)) != TRI_OK) return st;
   if (b->n_seqs > kMaxGrid) return TRI_ERR_RANGE;
   if (b->max_ctx_len > cache->max_seq || b->max_q_len > cache->max_seq) return TRI_ERR_RANGE;
   if (b->n_tokens > 0 && b->max_ctx_len >= cache->max_seq) return TRI_ERR_RANGE;

@@ -214,7 +214,11 @@ __global__ __launch_bounds__(256) void prologue_kernel(BatchDev b, KvDev kv, int
     const bool ok = in_batch && sl >= 0 && sl < kv.n_slots && row >= 0 && row < kv.max_seq &&
                     t >= q0 && t < q1;
     int prow = -1;
-    const int panel = ok ? kv_panel(kv, sl, row, prow) : -1;
+    int panel = ok ? kv_panel(kv, sl, row, prow) : -1;
+    if (kv.max_seq == 0) {  // the rows stay in the batch's order (an 8-bit cache takes them later)
+      panel = t;
+      prow = 0;
+    }
     tok_slot[t] = panel;
     tok_row[t] = panel >= 0 ? prow : -1;
   }

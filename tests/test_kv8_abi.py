@@ -150,6 +150,61 @@ def test_attention_refusals(lib):
     assert attend(lib, ws=FAKE + 16) == T.TRI_ERR_ALIGN
 
 
+def test_layer_refusals(lib):
+    w = T.LayerWeights(*[FAKE + (20 << 20) + 4096 * i for i in range(10)])
+
+    def layer(name="prefill", c=None, kv=None, b=None, x=FAKE + (8 << 20), out=FAKE + (9 << 20),
+              ws=FAKE + (10 << 20), ws_bytes=1 << 30):
+        c = c or cfg(dtype=T.TRI_BF16)
+        return getattr(lib, f"tri_layer_{name}_kv8")(
+            ctypes.byref(c), ctypes.byref(w), None if kv == 0 else ctypes.byref(kv or cache()),
+            ctypes.byref(b or batch()), x, out, None, None, ws, ws_bytes, None)
+
+    one = batch(n_seqs=2, n_tokens=2, max_q=1)
+    for name, b in (("prefill", None), ("decode", one)):
+        assert layer(name, b=b, kv=0) == T.TRI_ERR_NULL
+        assert layer(name, b=b, c=cfg(dtype=T.TRI_F32)) == T.TRI_ERR_UNSUPPORTED
+        assert layer(name, b=b, kv=cache(scale_rows=16)) == T.TRI_ERR_UNSUPPORTED
+        assert layer(name, b=b, kv=cache(v=FAKE + 4)) == T.TRI_ERR_ALIGN
+        assert layer(name, b=b, x=None) == T.TRI_ERR_NULL
+        assert layer(name, b=b, ws_bytes=4096) == T.TRI_ERR_WORKSPACE
+        assert layer(name, b=b, out=FAKE + (8 << 20)) == T.TRI_ERR_ALIAS
+    assert layer(b=batch(max_ctx=256)) == T.TRI_ERR_RANGE
+    assert layer("decode", b=batch()) == T.TRI_ERR_SHAPE                     # a chunk
+    n, m = ctypes.c_size_t(), ctypes.c_size_t()
+    size = lib.tri_workspace_size_kv8
+    assert size(ctypes.byref(cfg()), ctypes.byref(cache()), ctypes.byref(batch()), None) == T.TRI_ERR_NULL
+    assert size(ctypes.byref(cfg()), None, ctypes.byref(batch()), ctypes.byref(n)) == T.TRI_ERR_NULL
+    last = 0
+    for tokens in (5, 40, 200, 1000):                                       # never shrinks
+        b = batch(n_tokens=tokens, max_q=min(tokens, 256) // 2 + 1 if tokens < 500 else 256, n_seqs=8)
+        assert size(ctypes.byref(cfg()), ctypes.byref(cache()), ctypes.byref(b), ctypes.byref(n)) == T.TRI_OK
+        assert lib.tri_workspace_size(ctypes.byref(cfg()), ctypes.byref(b), ctypes.byref(m)) == T.TRI_OK
+        assert n.value > m.value and n.value >= last
+        last = n.value
+
+
+@pytest.mark.parametrize("mass", [False, True])
+def test_attention_workspace_never_shrinks(lib, mass):
+    """As tokens or the longest prefix grow, other scalars the same."""
+    kv = cache(max_seq=1 << 20, **({} if mass else {"mass": None}))
+    n = ctypes.c_size_t()
+
+    def size(b):
+        assert lib.tri_kv8_attention_workspace_size(ctypes.byref(cfg(n_q_heads=28, n_kv_heads=4, head_dim=128)),
+                                                    ctypes.byref(kv), ctypes.byref(b),
+                                                    ctypes.byref(n)) == T.TRI_OK
+        return n.value
+
+    for seqs, max_q in ((1, 1), (8, 1), (8, 300), (100, 7)):
+        tokens = sorted({min(seqs * max_q, max(seqs, max_q) + k) for k in range(0, 2500, 37)})
+        sizes = [size(batch(n_seqs=seqs, n_tokens=t, max_q=max_q, max_ctx=5000)) for t in tokens]
+        assert sizes == sorted(sizes)
+        sizes = [size(batch(n_seqs=seqs, n_tokens=tokens[0], max_q=max_q, max_ctx=c))
+                 for c in range(0, 100000, 777)]
+        assert sizes == sorted(sizes)
+
+
 def test_eviction_refusals(lib):
     assert select(lib, kv=cache(mass=None)) == T.TRI_ERR_NULL
     assert select(lib, plan=None) == T.TRI_ERR_NULL
