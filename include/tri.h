@@ -332,7 +332,9 @@ tri_status tri_rope(const tri_rope_table* table, const void* x, int64_t x_stride
  *  TRI_KV8_E4M3  code an 8-bit float of 4 exponent and 3 mantissa bits, at most 448
  * A scale is a power of two, 2^-100 or more, so that codes move to a larger one by a
  * shift.  A scale of NaN marks a block into which a value that is not finite was
- * appended: every value of it is NaN.
+ * appended: every value of it is NaN, and so are the output and the weights of a token
+ * that sees one of the block's rows, for the head's queries.  max_seq <= 2^23
+ * (TRI_ERR_RANGE).
  * The library reads n_q_heads, n_kv_heads, head_dim (64 or 128) and dtype
  * (TRI_BF16) of the tri_layer_config.                                           */
 typedef enum { TRI_KV8_INT8 = 0, TRI_KV8_E4M3 = 1 } tri_kv8_format;

@@ -15,6 +15,7 @@ tri_status tri::check_kv8_cache(const tri_kv8_cache* c) {
   if (!c) return TRI_ERR_NULL;
   if (!c->k || !c->v || !c->k_scale || !c->v_scale) return TRI_ERR_NULL;
   if (c->n_slots <= 0 || c->max_seq <= 0) return TRI_ERR_SHAPE;
+  if (c->max_seq > 1 << 23) return TRI_ERR_RANGE;  // a head's rows within 32-bit offsets
   if (c->format != TRI_KV8_INT8 && c->format != TRI_KV8_E4M3) return TRI_ERR_UNSUPPORTED;
   if (c->scale_rows != 32 && c->scale_rows != 64 && c->scale_rows != 128) return TRI_ERR_UNSUPPORTED;
   if (c->block_table) {

@@ -132,7 +132,9 @@ class Cache:
         2 e; the exponential and the sums of n terms by (n + 64) u; weights rounded to 11
         bits by 2^-11, or where they fall below 2^-14 of the largest weight (times its
         value's scale) by 2^-25 of it, 2^8 more while the running maximum lags; the
-        output's rounding is 2^-8 of it."""
+        output's rounding is 2^-8 of it.  A weight that is added to the mass may be lost
+        whole where it is below 2^-126, float32's least normal number: with a start of zero
+        the terms relative to it bound nothing there (exp(-96) is 2^-138 already)."""
         tokens, hq, D = q.shape
         u = 2.0 ** -24
         out, tol = np.full(q.shape, np.nan), np.zeros(q.shape)
@@ -166,7 +168,8 @@ class Cache:
                     mass[slot, h, :n] += p.sum(0)
                     mtol[slot, h, :n] += (few * p).sum(0)
             if mass is not None:  # and the sums over heads and tokens
-                mtol[slot, :, :n] += ((hq // k.shape[0]) * n_new + 2) * u * mass[slot, :, :n]
+                mtol[slot, :, :n] += ((hq // k.shape[0]) * n_new + 2) * (
+                    u * mass[slot, :, :n] + 2.0 ** -126)
         return out, tol, mass, mtol
 
     def select(self, batch, budget, n_first, n_recent):

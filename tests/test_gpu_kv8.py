@@ -324,6 +324,123 @@ def test_attention_skipped_sequences_and_strided_q():
             assert all((after[n][p] == before[n][p]).all() for n in before)
 
 
+@pytest.mark.parametrize("R", [32, 128])
+@pytest.mark.parametrize("max_seq", [1, 45, 77, 100])
+def test_odd_cache_lengths(max_seq, R):
+    """A contiguous cache that ends within a tile and a scale block, filled to its last row."""
+    cfg = config(4, 2, 64)
+    for fmt in FORMATS:
+        cache = make_cache(cfg, 3, max_seq, fmt, R, seed=max_seq)
+        batch = ([1, 0, 2], [max_seq - 1, 0, max_seq // 2], [1, max_seq, max_seq - max_seq // 2])
+        _, ref = run_append(cfg, cache, batch, seed=5)
+        same_cache(cache, ref)
+        run_attention(cfg, cache, batch)
+
+
+def test_rows_behind_the_last_sequence():
+    """Tokens that belong to no sequence: their outputs stay, nothing of them is appended."""
+    import torch
+    cfg = config(4, 2, 64)
+    for q in ([1, 1], [40, 1], [3, 70]):
+        cache = make_cache(cfg, 2, 256, seed=3)
+        db = T.DeviceBatch([1, 0], [30, 100], q)
+        n, db.n_tokens = db.n_tokens, db.n_tokens + 5
+        db.max_q_len = max(db.max_q_len, 6)  # as a caller with a padded batch would say
+        db.pos = torch.arange(db.n_tokens, dtype=torch.int32, device="cuda")
+        k = bf16(db.n_tokens, 2, 64, seed=1)
+        k[n:] = 1e30
+        ref = kv8_ref.Cache(cache)
+        T.kv8_append(cfg, cache, db, k, k)
+        ref.append(db.host, f64(k), f64(k), np.arange(db.n_tokens))
+        same_cache(cache, ref)
+        x = bf16(db.n_tokens, 4, 64, seed=2)
+        out = torch.full_like(x, 5.0)
+        want, tol, mass, mtol = ref.attention(db.host, f64(x))
+        T.kv8_attention(cfg, cache, db, x, out=out)
+        assert (np.abs(f64(out)[:n] - want[:n]) <= tol[:n]).all() and (out[n:] == 5).all()
+        ref.mass = mass
+        same_cache(cache, ref, mtol)
+
+
+@pytest.mark.parametrize("q", [[1, 1], [90, 1], [2, 64]])
+def test_cache_past_32_bits(q):
+    """The last slots of a cache whose codes pass 4 GiB, against a cache of those slots alone."""
+    import torch
+    cfg = config(16, 8, 128)
+    slots, max_seq = 34, 131072
+    big = T.KV8Cache.empty(cfg, slots, max_seq, "e4m3", 64, mass=True, stamp=True)
+    small = make_cache(cfg, 2, 2048, "e4m3", 64, seed=4)
+    assert big.k.numel() > 1 << 32
+    for name in ("k", "v", "mass", "stamp"):
+        a, b = getattr(big, name), getattr(small, name)
+        a.view(torch.uint8)[-2:, :, :2048] = b.view(torch.uint8) if a.dim() == 4 else 0
+        if a.dim() == 3:
+            a[-2:, :, :2048] = b
+    for name in ("k_scale", "v_scale"):
+        getattr(big, name)[-2:, :, :32] = getattr(small, name)
+    outs = []
+    for cache, off in ((big, slots - 2), (small, 0)):
+        db = T.DeviceBatch([off + 1, off], [1900, 700], q)
+        x = bf16(db.n_tokens, 16, 128, seed=2)
+        k = bf16(db.n_tokens, 8, 128, seed=3)
+        T.kv8_append(cfg, cache, db, k, k)
+        out, _ = T.kv8_attention(cfg, cache, db, x)
+        plan, _ = T.kv8_select(cfg, cache, db, 512, 4, 64)
+        T.kv8_move(cfg, cache, db, plan)
+        outs.append((out, plan))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    for name in ("k", "v", "mass", "stamp", "k_scale", "v_scale"):
+        a, b = getattr(big, name), getattr(small, name)
+        assert torch.equal(a[-2:, :, :b.shape[2]].view(torch.uint8), b.view(torch.uint8)), name
+
+
+def test_mixed_batch_on_the_side_stream():
+    """A batch whose single tokens may read 192 MiB runs them beside the chunk: the same
+    results as the sequences alone, in a graph too, and from two streams at once."""
+    import torch
+    cfg = config(4, 2, 64)
+    max_seq = 300032
+    cache = make_cache(cfg, 3, max_seq, "int8", 64, seed=1, stamp=False)
+    db = T.DeviceBatch([2, 0, 1], [5000, 200, 3000], [1, 80, 1])
+    db.max_ctx_len = 300000                      # a bound: the largest that may come
+    assert db.n_seqs * db.max_ctx_len * 2 * 64 * 2 >= 192 << 20
+    x = bf16(db.n_tokens, 4, 64, seed=2)
+    start, parts, t = cache.mass.clone(), [], 0
+    for s, c, n in zip([2, 0, 1], [5000, 200, 3000], [1, 80, 1]):
+        parts.append(T.kv8_attention(cfg, cache, T.DeviceBatch([s], [c], [n]), x[t:t + n])[0])
+        t += n
+    alone, mass = torch.cat(parts), cache.mass.clone()
+    close = lambda a, b: (a.float() - b.float()).abs().max() <= 2.0 ** -7 * b.float().abs().max()
+
+    def check(out, m):
+        assert close(out, alone) and close(m, mass)
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    caches = [T.KV8Cache(cache.k, cache.v, cache.k_scale, cache.v_scale, 64, mass=start.clone())
+              for _ in streams]
+    size = T.kv8_attention_workspace_size(cfg, caches[0], db)
+    bufs = [(torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty_like(x)) for _ in streams]
+    torch.cuda.synchronize()
+    for st, kv, (ws, out) in zip(streams, caches, bufs):       # two calls at once
+        T.kv8_attention(cfg, kv, db, x, out=out, workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    for kv, (_, out) in zip(caches, bufs):
+        check(out, kv.mass)
+    assert torch.equal(bufs[0][1], bufs[1][1]) and torch.equal(caches[0].mass, caches[1].mass)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=streams[0]):
+        T.kv8_attention(cfg, caches[0], db, x, out=bufs[0][1], workspace=bufs[0][0], stream=streams[0])
+    for i in range(3):
+        for kv, (_, out) in zip(caches, bufs):
+            kv.mass.copy_(start)
+            out.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        T.kv8_attention(cfg, caches[1], db, x, out=bufs[1][1], workspace=bufs[1][0], stream=streams[1])
+        torch.cuda.synchronize()
+        assert torch.equal(bufs[0][1], bufs[1][1]) and torch.equal(caches[0].mass, caches[1].mass), i
+
+
 def test_attention_repeats_bit_for_bit():
     import torch
     cfg = config(28, 4, 128)

@@ -110,6 +110,7 @@ def test_every_call_checks_config_cache_and_batch(lib):
         assert call(lib, kv=cache(format=2)) == T.TRI_ERR_UNSUPPORTED
         assert call(lib, kv=cache(scale_rows=48)) == T.TRI_ERR_UNSUPPORTED
         assert call(lib, kv=cache(n_slots=0)) == T.TRI_ERR_SHAPE
+        assert call(lib, kv=cache(max_seq=(1 << 23) + 1)) == T.TRI_ERR_RANGE
         assert call(lib, kv=cache(k=FAKE + 8)) == T.TRI_ERR_ALIGN
         assert call(lib, kv=cache(v_scale=FAKE + 2)) == T.TRI_ERR_ALIGN
         assert call(lib, kv=cache(mass=FAKE + 1)) == T.TRI_ERR_ALIGN
