@@ -334,7 +334,10 @@ tri_status tri_rope(const tri_rope_table* table, const void* x, int64_t x_stride
  * shift.  A scale of NaN marks a block into which a value that is not finite was
  * appended: every value of it is NaN, and so are the output and the weights of a token
  * that sees one of the block's rows, for the head's queries.  max_seq <= 2^23
- * (TRI_ERR_RANGE).
+ * (TRI_ERR_RANGE).  n_tokens may exceed cu_q[n_seqs]: tokens behind the last sequence
+ * are neither read nor written by the calls below that take a batch (but the layer's).
+ * A page that two sequences of a batch hold is read by both; no row of it may be
+ * appended or moved to, and `mass` must be NULL for the attention (its sums would race).
  * The library reads n_q_heads, n_kv_heads, head_dim (64 or 128) and dtype
  * (TRI_BF16) of the tri_layer_config.                                           */
 typedef enum { TRI_KV8_INT8 = 0, TRI_KV8_E4M3 = 1 } tri_kv8_format;
@@ -382,8 +385,11 @@ tri_status tri_kv8_append(const tri_layer_config* cfg, const tri_kv8_cache* cach
  * the KV head's query heads and the new tokens of the sequence (in one fixed order:
  * the same inputs give the same sums).  Codes are exact in the products; scores,
  * running maximum, sums and outputs are float32, attention weights rounded to 11 bits
- * for the product with the values.  Tokens of a skipped sequence (as in the append)
- * are left as they were.
+ * for the product with the values.  A weight counts in its output's denominator down
+ * to 2^(d - 126) of the largest, where the value scales of the rows that the token sees
+ * differ by up to 2^d (zeros have the scale 2^-100: d < 102, so 2^-24, while no value
+ * beside them passes 2^8).  Tokens of a skipped sequence (as in the append) are left as
+ * they were.
  * workspace: device, 256-byte aligned, of tri_kv8_attention_workspace_size bytes
  * (the cache's and the batch's host fields are read; it never shrinks as max_ctx_len or
  * n_tokens grows).                                                               */

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, 
                                                           bf16* __restrict__ O,
                                                           float* __restrict__ lse,
                                                           float* __restrict__ part, int nsplit,
-                                                          float scale_log2e) {
+                                                          int least, float scale_log2e) {
   constexpr int DS = D / 16, DB = D / 32;
   constexpr int NL = D / 64;  // 16-code loads of a thread, operand and tile
   __shared__ __align__(16) f16 sk[2][kKeys8 * D], sv[2][kKeys8 * D];
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, 
   rest /= Hkv;
   const int s = rest / nsplit, sp = rest - s * nsplit;
   int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2) return;
+  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < least) return;
   const int G = Hq / Hkv, rows = n * G, row0 = tile * kRows8;
   if (row0 >= rows) return;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -304,7 +304,8 @@ template <int D>
 __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
                                                             const float* __restrict__ part,
                                                             bf16* __restrict__ O,
-                                                            float* __restrict__ lse, int nsplit) {
+                                                            float* __restrict__ lse, int nsplit,
+                                                            int least) {
   constexpr int TPR = D / 4;
   const int t = blockIdx.x, h = blockIdx.y, G = Hq / Hkv, lane = threadIdx.x & 63;
   // the token's sequence: as many ends lie at or before it
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c
     s += __builtin_popcountll(__builtin_amdgcn_ballot_w64(j0 + lane < b.n_seqs && end <= t));
   }
   int q0, n, ctx, sl;
-  if (s >= b.n_seqs || !kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2 || t < q0 || t >= q0 + n) return;
+  if (s >= b.n_seqs || !kv8_seq(b, c, s, q0, n, ctx, sl) || n < least || t < q0 || t >= q0 + n) return;
   const int64_t plane = (int64_t)b.n_tokens * Hq * (D + 4);
   const int d = 4 * ((int)threadIdx.x % TPR);
   for (int g = (int)threadIdx.x / TPR; g < G; g += 256 / TPR) {
@@ -365,7 +366,7 @@ template <int D, bool FP8, int KG>
 __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
                                                                const bf16* __restrict__ Q, int64_t qs,
                                                                const float* __restrict__ lse,
-                                                               float scale_log2e) {
+                                                               int least, float scale_log2e) {
   constexpr int DS = D / 16, DC = D / 8;
   constexpr int RPB = 64 / DC;             // rows of a 1 KB load
   constexpr int RG = 8 / KG, kMassKeys = 32 * KG, kMassQ = 32 * RG;
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
   __shared__ float sums[RG][KG][32];
   const int s = blockIdx.z, h = blockIdx.y, key0 = blockIdx.x * kMassKeys;
   int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 2 || key0 >= ctx + n) return;
+  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < least || key0 >= ctx + n) return;
   const int G = Hq / Hkv, rows = n * G;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -515,7 +516,7 @@ size_t attn_kv8_workspace_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_head
 
 template <int D, bool FP8>
 static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv, const void* q,
-                             int64_t qs, void* out, char* ws, hipStream_t s) {
+                             int64_t qs, void* out, char* ws, int least, hipStream_t s) {
   const int sp = kv8_key_splits(b, Hq, Hkv), G = Hq / Hkv;
   float* lse = c.mass ? (float*)ws : nullptr;
   float* part = (float*)(ws + lse_bytes(b, c, Hq));
@@ -524,7 +525,7 @@ static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv
   if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
   auto go = [&](auto kernel) {
     kernel<<<(unsigned)wgs, 256, 0, s>>>(b, c, Hq, Hkv, (const bf16*)q, qs, (bf16*)out, lse, part, sp,
-                                         scale_log2e);
+                                         least, scale_log2e);
     return hipGetLastError();
   };
   hipError_t e;
@@ -533,7 +534,7 @@ static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv
   if (e != hipSuccess) return e;
   if (sp > 1) {
     attn_kv8_fold_kernel<D><<<dim3(b.n_tokens, Hkv), 256, 0, s>>>(
-        b, c, Hq, Hkv, part, (bf16*)out, lse, sp);
+        b, c, Hq, Hkv, part, (bf16*)out, lse, sp, least);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (c.mass) {
@@ -542,7 +543,7 @@ static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv
     auto weigh = [&](auto kg, auto kernel) {
       const int keys = 32 * decltype(kg)::value;
       kernel<<<dim3(cdiv(b.max_ctx_len + b.max_q_len, keys), Hkv, b.n_seqs), 512, 0, s>>>(
-          b, c, Hq, Hkv, (const bf16*)q, qs, lse, scale_log2e);
+          b, c, Hq, Hkv, (const bf16*)q, qs, lse, least, scale_log2e);
       return hipGetLastError();
     };
     if (wgs4 * 3 >= 2 * cu_count()) e = weigh(Int<4>{}, attn_kv8_mass_kernel<D, FP8, 4>);
@@ -567,20 +568,23 @@ hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q
   // workspace).  Fork and join cost about 20 us, so it pays from some 40 us of streaming:
   // 33 sequences up to 8192 rows (277 MB at most) take 173 us so and 190 in turn, up
   // to 4000 rows (135 MB) 87 us either way, 9 up to 600 45 and 28 us.
+  // Chunks that fill n_tokens at max_q_len each leave no single token, unless some of the
+  // tokens belong to no sequence: then one is a chunk of one.
+  const int least = (int64_t)b.n_seqs * b.max_q_len == b.n_tokens ? 1 : 2;
   Fork fork;
   hipError_t e = hipSuccess;
-  if ((int64_t)b.n_seqs * b.max_q_len != b.n_tokens) {
+  if (least == 2) {
     const int64_t bytes = (int64_t)b.n_seqs * (b.max_ctx_len + 1) * n_kv_heads * head_dim * 2;
     if (bytes >= kForkBytes) e = fork.begin(s);
     if (e == hipSuccess) e = singles(fork.stream ? fork.stream : s);
   }
   if (e == hipSuccess) {
     if (head_dim == 128)
-      e = fp8 ? run_flash8<128, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
-              : run_flash8<128, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
+      e = fp8 ? run_flash8<128, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, least, s)
+              : run_flash8<128, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, least, s);
     else
-      e = fp8 ? run_flash8<64, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s)
-              : run_flash8<64, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, s);
+      e = fp8 ? run_flash8<64, true>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, least, s)
+              : run_flash8<64, false>(b, c, n_q_heads, n_kv_heads, q, q_stride, out, w, least, s);
   }
   const hipError_t j = fork.end();
   return e != hipSuccess ? e : j;

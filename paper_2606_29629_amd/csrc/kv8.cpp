@@ -208,6 +208,7 @@ tri_status tri_kv8_attention_workspace_size(const tri_layer_config* cfg,
   tri_status st = check_call(cfg, cache, b);
   if (st == TRI_OK) st = check_group(cfg);
   if (st != TRI_OK) return st;
+  if ((int64_t)b->n_tokens * cfg->n_q_heads > 0x7fffffff) return TRI_ERR_RANGE;
   *bytes = b->n_tokens == 0 ? 0 : attn_kv8_workspace_bytes(batch_dev(b), kv8_dev(cache), cfg->n_q_heads,
                                                            cfg->n_kv_heads, cfg->head_dim);
   return TRI_OK;

@@ -341,11 +341,11 @@ def test_rows_behind_the_last_sequence():
     """Tokens that belong to no sequence: their outputs stay, nothing of them is appended."""
     import torch
     cfg = config(4, 2, 64)
-    for q in ([1, 1], [40, 1], [3, 70]):
+    for q, pad in (([1, 1], 5), ([40, 1], 5), ([3, 70], 5), ([1, 3], 2), ([70, 1], 69), ([1, 1], 2)):
         cache = make_cache(cfg, 2, 256, seed=3)
         db = T.DeviceBatch([1, 0], [30, 100], q)
-        n, db.n_tokens = db.n_tokens, db.n_tokens + 5
-        db.max_q_len = max(db.max_q_len, 6)  # as a caller with a padded batch would say
+        n, db.n_tokens = db.n_tokens, db.n_tokens + pad
+        db.max_q_len = max(db.max_q_len, -(-db.n_tokens // 2))
         db.pos = torch.arange(db.n_tokens, dtype=torch.int32, device="cuda")
         k = bf16(db.n_tokens, 2, 64, seed=1)
         k[n:] = 1e30
@@ -360,6 +360,18 @@ def test_rows_behind_the_last_sequence():
         assert (np.abs(f64(out)[:n] - want[:n]) <= tol[:n]).all() and (out[n:] == 5).all()
         ref.mass = mass
         same_cache(cache, ref, mtol)
+
+
+def test_value_scales_far_apart():
+    """A block of zeros (scale 2^-100) beside values of up to 2^8: their rows count in full."""
+    cfg = config(4, 2, 64)
+    for batch in (([0, 1], [99, 64], [1, 1]), ([0, 1], [99, 64], [3, 40])):
+        cache = make_cache(cfg, 2, 256, seed=3)
+        cache.v[:, :, :64] = 0
+        cache.v_scale[:, :, :2] = 2.0 ** -100
+        cache.v_scale[:, :, 2:] = 2.0
+        cache.k_scale.fill_(2.0 ** -9)
+        run_attention(cfg, cache, batch)
 
 
 @pytest.mark.parametrize("q", [[1, 1], [90, 1], [2, 64]])

@@ -206,6 +206,12 @@ def test_attention_workspace_never_shrinks(lib, mass):
         assert sizes == sorted(sizes)
 
 
+def test_attention_rows_of_heads_within_32_bits(lib):
+    c, b = cfg(n_q_heads=64, n_kv_heads=2), batch(n_seqs=60000, n_tokens=60000 * 2000, max_q=2000)
+    kv = cache(max_seq=4096)
+    assert attend(lib, c=c, kv=kv, b=b) == T.TRI_ERR_RANGE
+
+
 def test_eviction_refusals(lib):
     assert select(lib, kv=cache(mass=None)) == T.TRI_ERR_NULL
     assert select(lib, plan=None) == T.TRI_ERR_NULL
