@@ -42,6 +42,47 @@ __device__ __forceinline__ void stage_place(int i, int& row, int& chunk) {
   }
 }
 
+// The sequences' pieces laid end to end (those of `least` tokens or more; `pieces` of the
+// tokens and cached rows): the sequence of piece `item`, its fields, and which of its pieces
+// it is, counted from the last if BACK; false past the end.  Every wave looks for itself, 64
+// sequences at a time.  So the workgroups that have work come first: with a grid of the
+// longest chunk's pieces for every sequence, those without held up the others, each for the
+// time of its loads (8 prompts of 500 to 2048 tokens, 28/4 heads of 128: 243 us, 129 so; 512
+// tokens beside 32 single ones, 14300 of 14800 without: 171 us, 141 so).
+template <typename F>
+__device__ __forceinline__ bool kv8_piece(const BatchDev& b, const Kv8Dev& c, int least, int item,
+                                          F&& pieces, int& s, int& piece, int& count, int& q0, int& n,
+                                          int& ctx, int& sl) {
+  const int lane = threadIdx.x & 63;
+  for (int j0 = 0; j0 < b.n_seqs; j0 += 64) {
+    int lq, ln, lc, ls;
+    const bool ok = kv8_seq(b, c, min(j0 + lane, b.n_seqs - 1), lq, ln, lc, ls) && ln >= least &&
+                    j0 + lane < b.n_seqs;
+    const int mine = ok ? pieces(ln, lc) : 0;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += v;
+    }
+    const uint64_t past = __builtin_amdgcn_ballot_w64(upto > item);
+    if (past == 0) {
+      item -= __builtin_amdgcn_readlane(upto, 63);
+      continue;
+    }
+    const int at = __builtin_ctzll(past);
+    s = j0 + at;
+    count = __builtin_amdgcn_readlane(mine, at);
+    piece = item - (__builtin_amdgcn_readlane(upto, at) - count);
+    q0 = __builtin_amdgcn_readlane(lq, at);
+    n = __builtin_amdgcn_readlane(ln, at);
+    ctx = __builtin_amdgcn_readlane(lc, at);
+    sl = __builtin_amdgcn_readlane(ls, at);
+    return true;
+  }
+  return false;
+}
+
 template <int D, bool FP8, bool PAGED, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
                                                           const bf16* __restrict__ Q, int64_t qs,
@@ -53,16 +94,22 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_kernel(BatchDev b, Kv8Dev c, 
   constexpr int NL = D / 64;  // 16-code loads of a thread, operand and tile
   __shared__ __align__(16) f16 sk[2][kKeys8 * D], sv[2][kKeys8 * D];
 
-  // the rows with the most keys first, over all heads and sequences
-  const int per = Hkv * b.n_seqs * nsplit;
-  const int tile = (int)(gridDim.x / per) - 1 - (int)(blockIdx.x / per);
-  int rest = blockIdx.x % per;
-  const int h = rest % Hkv;
-  rest /= Hkv;
-  const int s = rest / nsplit, sp = rest - s * nsplit;
-  int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < least) return;
-  const int G = Hq / Hkv, rows = n * G, row0 = tile * kRows8;
+  // Heads, then splits, then the row tiles, those with the most keys first: over all sequences
+  // where they are equal chunks (least = 1; 8 of 2048 tokens: 292 us, in turn 308), else
+  // sequence by sequence.
+  const int per = Hkv * nsplit, h = (int)(blockIdx.x % per) % Hkv, sp = (int)(blockIdx.x % per) / Hkv;
+  const int G = Hq / Hkv, item = (int)(blockIdx.x / per);
+  int s, tile, tiles, q0, n, ctx, sl;
+  if (least == 1) {
+    s = item % b.n_seqs;
+    tile = item / b.n_seqs;
+    tiles = (int)(gridDim.x / per) / b.n_seqs;
+    if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < 1) return;
+  } else if (!kv8_piece(b, c, least, item, [&](int tokens, int) { return cdiv(tokens * G, kRows8); }, s,
+                        tile, tiles, q0, n, ctx, sl)) {
+    return;
+  }
+  const int rows = n * G, row0 = (tiles - 1 - tile) * kRows8;
   if (row0 >= rows) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -360,8 +407,8 @@ __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c
 // SIMD's two waves cover each other's waits.  Every sum has one order.  Fewer groups make
 // more workgroups of fewer steps that read the queries more often: KG = 4 where that fills
 // two thirds of the CUs, 2 down to a third, else 1 (whole calls with 4, 2 and 1: 4 chunks of
-// 300 to 900 tokens, 2 KV heads of 64, 66 workgroups at 4: 97, 73, 62 us; 200 tokens at 2000
-// beside single ones, 4 heads of 128, 144: 72, 65, 73; 8 x 1024, 256: 174, 186, 273).
+// 300 to 900 tokens, 2 KV heads of 64, 66 workgroups at 4: 88, 63, 52 us; 200 tokens at 2000
+// beside single ones, 4 heads of 128, 144: 62, 55, 62; 8 x 1024, 256: 165, 195, 266).
 template <int D, bool FP8, int KG>
 __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
                                                                const bf16* __restrict__ Q, int64_t qs,
@@ -403,19 +450,35 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
       }
     }
   }
-  // row tiles from the first that sees key0
+  // Row tiles from the first that sees key0.  A tile's first row is head `rem0` of token tok0;
+  // both go on by a tile's rows, and a row's place in the tile takes one comparison.
   const int rt_lo = max(0, key0 - ctx) * G / kMassQ, rt_hi = cdiv(rows, kMassQ);
-  auto gload = [&](int rt, auto buf) {
+  const int tok_step = kMassQ / G, rem_step = kMassQ - tok_step * G;
+  int tok0 = rt_lo * kMassQ / G, rem0 = rt_lo * kMassQ - tok0 * G;  // of the tile loaded next
+  int head_of[NL];
+  uint32_t place[NL];
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    const int r = (wave + 8 * j) * RPB + lane / DC, t = r / G;
+    head_of[j] = r - t * G;
+    place[j] = (uint32_t)(t * (int)qs + head_of[j] * D + kv_chunk<D>(lane % DC, r) * 8) * 2;
+  }
+  auto gload = [&](auto buf) {
     bf16* dst = decltype(buf)::value ? sq1 : sq0;
-    const int tok0 = rt * kMassQ / G;
-    const auto rq = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(Q + (int64_t)(q0 + tok0) * qs + (int64_t)h * G * D), (short)0, 0x7fffffff, 0x00020000);
+    // (rows past the last read as zero)
+    const int64_t bytes = ((int64_t)(n - 1 - tok0) * qs + G * D) * 2;
+    const auto rq = __builtin_amdgcn_make_buffer_rsrc((void*)(Q + (int64_t)(q0 + tok0) * qs + (int64_t)h * G * D),
+                                                      (short)0, (int)min(bytes, (int64_t)0x7fffffff), 0x00020000);
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const int blk = wave + 8 * j, r = blk * RPB + lane / DC;
-      const int row = min(rt * kMassQ + r, rows - 1), tok = row / G;
-      const uint32_t off = (uint32_t)((tok - tok0) * (int)qs + (row - tok * G) * D + kv_chunk<D>(lane % DC, r) * 8) * 2;
-      buffer_load_lds16(rq, dst + blk * 512, off, 0);
+      const uint32_t off = place[j] + rem0 * D * 2 + (head_of[j] + rem0 >= G ? (uint32_t)((int)qs - G * D) * 2 : 0u);
+      buffer_load_lds16(rq, dst + (wave + 8 * j) * 512, off, 0);
+    }
+    tok0 += tok_step;
+    rem0 += rem_step;
+    if (rem0 >= G) {
+      rem0 -= G;
+      ++tok0;
     }
   };
   float acc[16];
@@ -426,40 +489,55 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
     const int row = rt * kMassQ + 32 * rg + lr;
     return row < rows ? lp[row] : INFINITY;
   };
-  float off_next = lse_of(rt_lo);
-  gload(rt_lo, Int<0>{});
+  // Both matrix product and exponentials take most of a step: those of the tile before run
+  // under the product of this one.  (rows past the end: 2^-inf)
+  float off_next = lse_of(rt_lo), off_old = INFINITY;
+  f32x16 old = f32x16{0.f};
+  auto weigh = [&](auto e_) {
+    constexpr int e = decltype(e_)::value;
+    acc[e] += __builtin_amdgcn_exp2f(fmaf(old[e], kf, -off_old));
+  };
+  int tok_of = tok0;  // first token of the tile at work
+  gload(Int<0>{});
   auto step = [&](int rt, auto buf) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const float off = off_next;
+    const int first = tok_of;
+    tok_of = tok0;
     if (rt + 1 < rt_hi) {
       off_next = lse_of(rt + 1);  // (before the rows: loads come back in order)
-      gload(rt + 1, Int<1 - decltype(buf)::value>{});
+      gload(Int<1 - decltype(buf)::value>{});
     }
     const bf16* qb = decltype(buf)::value ? sq1 : sq0;
-    const int r = 32 * rg + lr, row = rt * kMassQ + r;
-    const int qpos = ctx + min(row, rows - 1) / G;
+    const int r = 32 * rg + lr;
+    constexpr int LA = 3;
+    bf16x8 qf[LA + 1];
+    auto qread = [&](int t) { return *(const bf16x8*)&qb[r * D + kv_chunk<D>(2 * t + lg, r) * 8]; };
+#pragma unroll
+    for (int t = 0; t < LA; ++t) qf[t] = qread(t);
     f32x16 sc = f32x16{0.f};
+    each<DS>([&](auto t_) {
+      constexpr int t = decltype(t_)::value, PER = 16 / DS;
+      if constexpr (t + LA < DS) qf[(t + LA) % (LA + 1)] = qread(t + LA);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kreg[t], qf[t % (LA + 1)], sc, 0, 0, 0);
+      each<PER>([&](auto j) { weigh(Int<t * PER + decltype(j)::value>{}); });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (wkey + 31 > ctx + first) {  // some row may not see some key
+      const int qpos = ctx + min(rt * kMassQ + r, rows - 1) / G;
 #pragma unroll
-    for (int t = 0; t < DS; ++t)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          kreg[t], *(const bf16x8*)&qb[r * D + kv_chunk<D>(2 * t + lg, r) * 8], sc, 0, 0, 0);
-    // (rows past the end: 2^-inf)
-    if (wkey + 31 > ctx + rt * kMassQ / G) {  // some row may not see some key
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(sc[e], kf, -off));
-        acc[e] += wkey + (e & 3) + 8 * (e >> 2) + 4 * lg <= qpos ? w : 0.f;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[e] += __builtin_amdgcn_exp2f(fmaf(sc[e], kf, -off));
+      for (int e = 0; e < 16; ++e)
+        if (wkey + (e & 3) + 8 * (e >> 2) + 4 * lg > qpos) sc[e] = -INFINITY;
     }
+    old = sc;
+    off_old = off;
   };
   for (int rt = rt_lo; rt < rt_hi; rt += 2) {
     step(rt, Int<0>{});
     if (rt + 1 < rt_hi) step(rt + 1, Int<1>{});
   }
+  each<16>(weigh);
   // the group's waves: their sums through LDS, added in order
   float* mp = c.mass + kv8_row_at(c, Hkv, max(panel, 0), h, prow);
 #pragma unroll
@@ -479,9 +557,9 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
 
 // Key-range splits: doubled while the workgroups fit one to a CU and a split keeps 4 tiles of
 // the longest range, or two to a CU and it keeps 8.  (512 tokens at 6144 beside 32 single
-// ones, 28/4 heads of 128, 112 workgroups unsplit: 190 us with two splits, 173 with four; 40
-// tokens at 6000, 12: 37 us with eight, 31 with sixteen; 500 at 1000 beside single ones, 14/2
-// heads of 64, 60: 31 us with four, 37 with eight.)
+// ones, 28/4 heads of 128, 112 workgroups unsplit: 148 us with two splits, 141 with four, 176
+// with eight; 40 tokens at 6000, 12: 35 us with eight, 31 with sixteen, 34 with 32; 500 at 1000
+// beside single ones, 14/2 heads of 64, 60: 28 us with two, 24 with four, 28 with eight.)
 static int kv8_key_splits(const BatchDev& b, int n_q_heads, int n_kv_heads) {
   const int64_t wgs = (int64_t)cdiv(b.n_tokens * (n_q_heads / n_kv_heads), kRows8) * n_kv_heads;
   const int tiles = cdiv(b.max_ctx_len + b.max_q_len, kKeys8), cus = cu_count();
@@ -521,7 +599,11 @@ static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv
   float* lse = c.mass ? (float*)ws : nullptr;
   float* part = (float*)(ws + lse_bytes(b, c, Hq));
   const float scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
-  const int64_t wgs = (int64_t)cdiv(b.max_q_len * G, kRows8) * Hkv * b.n_seqs * sp;
+  // row tiles: at most one of a sequence's is in part empty
+  const int64_t chunks = std::min(b.n_seqs, b.n_tokens / least);
+  const int64_t tiles = std::min(chunks * cdiv(b.max_q_len * G, kRows8),
+                                 ((int64_t)b.n_tokens * G + chunks * (kRows8 - 1)) / kRows8);
+  const int64_t wgs = (least == 1 ? (int64_t)b.n_seqs * cdiv(b.max_q_len * G, kRows8) : tiles) * Hkv * sp;
   if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
   auto go = [&](auto kernel) {
     kernel<<<(unsigned)wgs, 256, 0, s>>>(b, c, Hq, Hkv, (const bf16*)q, qs, (bf16*)out, lse, part, sp,
@@ -566,8 +648,8 @@ hipError_t launch_attn_kv8(const BatchDev& b, const Kv8Dev& c, bool fp8, int n_q
   // Single tokens beside chunks, memory-bound beside compute-bound: on the side stream where
   // their stream is long enough (other output rows, other weights' rows, another part of the
   // workspace).  Fork and join cost about 20 us, so it pays from some 40 us of streaming:
-  // 33 sequences up to 8192 rows (277 MB at most) take 173 us so and 190 in turn, up
-  // to 4000 rows (135 MB) 87 us either way, 9 up to 600 45 and 28 us.
+  // 33 sequences up to 8192 rows (277 MB at most) take 139 us so and 171 in turn, up to 4000
+  // rows (135 MB) 70 and 76 (on an idle GPU 98 and 91), 9 up to 600 47 and 25.
   // Chunks that fill n_tokens at max_q_len each leave no single token, unless some of the
   // tokens belong to no sequence: then one is a chunk of one.
   const int least = (int64_t)b.n_seqs * b.max_q_len == b.n_tokens ? 1 : 2;

@@ -224,7 +224,7 @@ tri_status tri_kv8_attention(const tri_layer_config* cfg, const tri_kv8_cache* c
   if (!q || !out || !b->cu_q || !b->ctx_len || !b->slot) return TRI_ERR_NULL;
   const int64_t width = (int64_t)cfg->n_q_heads * cfg->head_dim;
   if (q_stride < width) return TRI_ERR_SHAPE;
-  if (q_stride > 1 << 23) return TRI_ERR_RANGE;  // 32-bit offsets within a tile of rows
+  if (q_stride > 1 << 22) return TRI_ERR_RANGE;  // 31-bit byte offsets within a tile of rows
   if (q_stride % 8 || !aligned16(q) || !aligned16(out)) return TRI_ERR_ALIGN;
   if (need > 0 && (!ws || ws_bytes < need)) return TRI_ERR_WORKSPACE;
   if (need > 0 && ((uintptr_t)ws & (kAlign - 1)) != 0) return TRI_ERR_ALIGN;
