@@ -373,23 +373,27 @@ __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c
     const float* pp = part + at * (D + 4);
     float M = -INFINITY, L = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int j0 = 0; j0 < ns; j0 += 8) {
-      f32x2 ml[8];
-      f32x4 a[8];
+    for (int j0 = 0; j0 < ns; j0 += 4) {
+      f32x2 ml[4];
+      f32x4 a[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {  // (splits past the last are loaded again and dropped)
+      for (int j = 0; j < 4; ++j) {  // (splits past the last are loaded again and dropped)
         const float* pj = pp + min(j0 + j, ns - 1) * plane;
         ml[j] = *(const f32x2*)(pj + D);
         a[j] = *(const f32x4*)(pj + d);
       }
+      const float Mn = fmaxf(max3f(M, ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+      const float at_max = Mn == -INFINITY ? 0.f : Mn;  // (no key visible so far: all 0)
+      const float x = __builtin_amdgcn_exp2f(M - at_max);
+      M = Mn;
+      L *= x;
+      o *= x;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (j0 + j >= ns || (ml[j][0] == -INFINITY && ml[j][1] == 0.f)) continue;  // no key visible
-        const float Mn = fmaxf(M, ml[j][0]);
-        const float x = M == -INFINITY ? 0.f : exp2f(M - Mn), w = exp2f(ml[j][0] - Mn);
-        L = L * x + ml[j][1] * w;
-        o = o * x + a[j] * w;
-        M = Mn;
+      for (int j = 0; j < 4; ++j) {
+        if (j0 + j >= ns) continue;
+        const float w = __builtin_amdgcn_exp2f(ml[j][0] - at_max);
+        L = fmaf(ml[j][1], w, L);
+        o += a[j] * w;
       }
     }
     bf16x4 o4;
