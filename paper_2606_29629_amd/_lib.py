@@ -298,6 +298,7 @@ def _layer(fn_name, cfg, w, cache, batch, x, out, workspace, route_idx, route_w,
     if isinstance(cache, KV8Cache):
         if (cfg.n_kv_heads, cfg.head_dim) != (cache.n_kv_heads, cache.head_dim):
             raise ValueError(f"{fn_name}: the cache has {cache.n_kv_heads} heads of {cache.head_dim}")
+        _on_gpu(fn_name, stream, x, out, cache.k, batch.slot, workspace)
         fn_name, kc = fn_name + "_kv8", cache.struct()
     else:
         kc = kv_struct(cache)
@@ -420,12 +421,24 @@ def _on_gpu(what: str, stream, first, *others) -> Optional[int]:
     return getattr(stream, "cuda_stream", stream)
 
 
+def _empty(stream, shape, dtype, device):
+    """torch.empty from the memory of the stream that the call runs on: what is freed when
+    the call returns is not handed to another stream while the kernels still use it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def rope(table: RopeTable, x, pos, out=None, stream=None):
     """x [tokens, heads, head_dim] (bf16 or float32, tokens any stride apart) with its
     heads rotated to int32 positions pos [tokens] (tri_rope); out=x: in place."""
     import torch
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _empty(stream, x.shape, x.dtype, x.device)
     f32 = x.dtype == torch.float32
     if not f32 and x.dtype != torch.bfloat16 or out.dtype != x.dtype:
         raise ValueError(f"rope: bf16 or float32 in and out, got {x.dtype} and {out.dtype}")
@@ -555,12 +568,11 @@ def kv8_attention(cfg, cache: KV8Cache, batch, q, out=None, workspace=None, stre
     if n != batch.n_tokens or heads != cfg.n_q_heads or q.dtype != torch.bfloat16:
         raise ValueError(f"kv8_attention: q is bf16 [{batch.n_tokens}, {cfg.n_q_heads}, {cfg.head_dim}]")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _empty(stream, q.shape, q.dtype, q.device)
     if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
         raise ValueError(f"kv8_attention: out is contiguous bf16 {tuple(q.shape)}")
     if workspace is None:
-        workspace = torch.empty(kv8_attention_workspace_size(cfg, cache, batch),
-                                dtype=torch.uint8, device=q.device)
+        workspace = _empty(stream, kv8_attention_workspace_size(cfg, cache, batch), torch.uint8, q.device)
     c, kv, b, stream = _kv8("kv8_attention", cfg, cache, batch, stream, q, out, workspace)
     st = lib().tri_kv8_attention(c, kv, b, q.data_ptr(), stride, out.data_ptr(), workspace.data_ptr(),
                                  workspace.nbytes, stream)
@@ -590,15 +602,15 @@ def kv8_select(cfg, cache: KV8Cache, batch, budget: int, n_first: int = 0, n_rec
     import torch
     n = batch.n_seqs
     if plan is None:
-        plan = torch.empty((n, cfg.n_kv_heads, budget), dtype=torch.int32, device=cache.k.device)
+        plan = _empty(stream, (n, cfg.n_kv_heads, budget), torch.int32, cache.k.device)
     if new_len is None:
-        new_len = torch.empty(n, dtype=torch.int32, device=cache.k.device)
+        new_len = _empty(stream, n, torch.int32, cache.k.device)
     _plan("kv8_select", plan, n, cfg.n_kv_heads, budget)
     if new_len.dtype != torch.int32 or new_len.numel() != n or not new_len.is_contiguous():
         raise ValueError(f"kv8_select: new_len is a contiguous int32 [{n}]")
     if workspace is None and batch.max_ctx_len + batch.max_q_len > 16384:  # (else none is needed)
-        workspace = torch.empty(kv8_select_workspace_size(cfg, cache, batch, budget),
-                                dtype=torch.uint8, device=plan.device)
+        workspace = _empty(stream, kv8_select_workspace_size(cfg, cache, batch, budget), torch.uint8,
+                           plan.device)
     c, kv, b, stream = _kv8("kv8_select", cfg, cache, batch, stream, plan, new_len, workspace)
     st = lib().tri_kv8_select(c, kv, b, budget, n_first, n_recent, plan.data_ptr(),
                               new_len.data_ptr(), _ptr(workspace),

@@ -406,6 +406,25 @@ def test_cache_past_32_bits(q):
         assert torch.equal(a[-2:, :, :b.shape[2]].view(torch.uint8), b.view(torch.uint8)), name
 
 
+def test_memory_of_the_callers_stream():
+    """A workspace that the call allocates and drops comes from its own stream's memory: what
+    the current stream allocates right after does not reach into it."""
+    import torch
+    cfg = config(4, 2, 64)
+    n = 200000
+    cache = make_cache(cfg, 1, n + 64, "int8", 64, seed=1)
+    db = T.DeviceBatch([0], [n - 1], [1])
+    want = T.kv8_select(cfg, cache, db, 64 * 1024, 4, 64)
+    stream = torch.cuda.Stream()
+    for given in (stream, stream.cuda_stream):
+        torch.cuda.synchronize()
+        got = T.kv8_select(cfg, cache, db, 64 * 1024, 4, 64, stream=given)
+        junk = [torch.full((size,), 77, dtype=torch.uint8, device="cuda")
+                for size in (T.kv8_select_workspace_size(cfg, cache, db, 64 * 1024),) * 8]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), junk[0]
+
+
 def test_mixed_batch_on_the_side_stream():
     """A batch whose single tokens may read 192 MiB runs them beside the chunk: the same
     results as the sequences alone, in a graph too, and from two streams at once."""

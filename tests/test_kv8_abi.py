@@ -311,6 +311,8 @@ def test_binding_refuses_before_the_call():
     x = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="current GPU"):                     # host tensors
         T.kv8_append(c, kv, b, x, x)
+    with pytest.raises(ValueError, match="current GPU"):
+        T.layer_prefill(c, {}, kv, b, torch.zeros(3, 256, dtype=torch.bfloat16))
     with pytest.raises(ValueError):                                          # a token too few
         T.kv8_append(c, kv, b, x[:2], x[:2])
     with pytest.raises(ValueError):
