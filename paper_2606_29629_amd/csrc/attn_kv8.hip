@@ -413,9 +413,15 @@ __global__ __launch_bounds__(256) void attn_kv8_fold_kernel(BatchDev b, Kv8Dev c
 // two thirds of the CUs, 2 down to a third, else 1 (whole calls with 4, 2 and 1: 4 chunks of
 // 300 to 900 tokens, 2 KV heads of 64, 66 workgroups at 4: 88, 63, 52 us; 200 tokens at 2000
 // beside single ones, 4 heads of 128, 144: 62, 55, 62; 8 x 1024, 256: 165, 195, 266).
-template <int D, bool FP8, int KG>
-__global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int Hq, int Hkv,
-                                                               const bf16* __restrict__ Q, int64_t qs,
+//
+// Workgroups: a grid of every sequence's most pieces, or, where that is more than 16 per CU,
+// four per CU that go through the pieces there are (LIST): most of a large grid has no keys,
+// and passes through the CUs that the others leave (512 tokens at 6144 beside 32 single ones:
+// 138 us and 137, beside 128: 218 and 202; 256 at 1000 beside 256: 146 and 127; a grid of 9
+// per CU: 54 and 55).
+template <int D, bool FP8, int KG, bool LIST>
+__global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8Dev c, int q_heads, int kv_heads,
+                                                               const bf16* __restrict__ Q, int64_t q_stride,
                                                                const float* __restrict__ lse,
                                                                int least, float scale_log2e) {
   constexpr int DS = D / 16, DC = D / 8;
@@ -424,139 +430,162 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
   constexpr int NL = kMassQ / RPB / 8;     // such loads of a wave and tile
   __shared__ __align__(16) bf16 sq0[kMassQ * D], sq1[kMassQ * D];
   __shared__ float sums[RG][KG][32];
-  const int s = blockIdx.z, h = blockIdx.y, key0 = blockIdx.x * kMassKeys;
-  int q0, n, ctx, sl;
-  if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < least || key0 >= ctx + n) return;
-  const int G = Hq / Hkv, rows = n * G;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 31, lg = lane >> 5;
-  // codes of this wave's 32 keys: lane key lr, values 16 t + 8 lg ...
-  const int kg = wave % KG, rg = wave / KG, wkey = key0 + 32 * kg;
-  int prow = 0;
-  const int panel = wkey < ctx + n ? kv_panel(c.kv, sl, wkey, prow) : -1;
-  const int live = panel < 0 ? 0 : min(32, ctx + n - wkey);
-  float kf = 0.f;
-  bf16x8 kreg[DS];
-  {
-    const int64_t head = (int64_t)max(panel, 0) * Hkv + h;
-    if (live > 0) kf = c.k_scale[head * c.scales_per_panel() + (prow >> c.scale_shift)] * scale_log2e;
-    const auto rk = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(c.k + (head * c.kv.panel_rows() + prow) * D), (short)0, live * D, 0x00020000);
+  int item = blockIdx.x;
+  do {
+    // (formed anew for every item: what depends on these is not kept across items in registers)
+    int Hq = q_heads, Hkv = kv_heads, tid = threadIdx.x;
+    int64_t qs = q_stride;
+    if constexpr (LIST) asm volatile("" : "+s"(Hq), "+s"(Hkv), "+s"(qs), "+v"(tid));
+    int h, s, piece, q0, n, ctx, sl;
+    if constexpr (LIST) {
+      int pieces;
+      h = item % Hkv;
+      if (!kv8_piece(b, c, least, item / Hkv,
+                     [&](int tokens, int held) { return cdiv(held + tokens, kMassKeys); }, s, piece, pieces, q0,
+                     n, ctx, sl))
+        return;
+    } else {
+      s = blockIdx.z, h = blockIdx.y, piece = blockIdx.x;
+      if (!kv8_seq(b, c, s, q0, n, ctx, sl) || n < least || piece * kMassKeys >= ctx + n) return;
+    }
+    const int key0 = piece * kMassKeys;
+    const int G = Hq / Hkv, rows = n * G;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lr = lane & 31, lg = lane >> 5;
+    // codes of this wave's 32 keys: lane key lr, values 16 t + 8 lg ...
+    const int kg = wave % KG, rg = wave / KG, wkey = key0 + 32 * kg;
+    int prow = 0;
+    const int panel = wkey < ctx + n ? kv_panel(c.kv, sl, wkey, prow) : -1;
+    const int live = panel < 0 ? 0 : min(32, ctx + n - wkey);
+    float kf = 0.f;
+    bf16x8 kreg[DS];
+    {
+      const int64_t head = (int64_t)max(panel, 0) * Hkv + h;
+      if (live > 0) kf = c.k_scale[head * c.scales_per_panel() + (prow >> c.scale_shift)] * scale_log2e;
+      const auto rk = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)(c.k + (head * c.kv.panel_rows() + prow) * D), (short)0, live * D, 0x00020000);
 #pragma unroll
-    for (int t = 0; t < DS; ++t) {
-      const auto w = __builtin_amdgcn_raw_buffer_load_b64(rk, lr * D + 16 * t + 8 * lg, 0, 0);
-      const f32x4 lo = kv8_decode4<FP8>(w[0]), hi = kv8_decode4<FP8>(w[1]);
+      for (int t = 0; t < DS; ++t) {
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(rk, lr * D + 16 * t + 8 * lg, 0, 0);
+        const f32x4 lo = kv8_decode4<FP8>(w[0]), hi = kv8_decode4<FP8>(w[1]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        kreg[t][e] = f2bf(lo[e]);
-        kreg[t][4 + e] = f2bf(hi[e]);
+        for (int e = 0; e < 4; ++e) {
+          kreg[t][e] = f2bf(lo[e]);
+          kreg[t][4 + e] = f2bf(hi[e]);
+        }
       }
     }
-  }
-  // Row tiles from the first that sees key0.  A tile's first row is head `rem0` of token tok0;
-  // both go on by a tile's rows, and a row's place in the tile takes one comparison.
-  const int rt_lo = max(0, key0 - ctx) * G / kMassQ, rt_hi = cdiv(rows, kMassQ);
-  const int tok_step = kMassQ / G, rem_step = kMassQ - tok_step * G;
-  int tok0 = rt_lo * kMassQ / G, rem0 = rt_lo * kMassQ - tok0 * G;  // of the tile loaded next
-  int head_of[NL];
-  uint32_t place[NL];
-#pragma unroll
-  for (int j = 0; j < NL; ++j) {
-    const int r = (wave + 8 * j) * RPB + lane / DC, t = r / G;
-    head_of[j] = r - t * G;
-    place[j] = (uint32_t)(t * (int)qs + head_of[j] * D + kv_chunk<D>(lane % DC, r) * 8) * 2;
-  }
-  auto gload = [&](auto buf) {
-    bf16* dst = decltype(buf)::value ? sq1 : sq0;
-    // (rows past the last read as zero)
-    const int64_t bytes = ((int64_t)(n - 1 - tok0) * qs + G * D) * 2;
-    const auto rq = __builtin_amdgcn_make_buffer_rsrc((void*)(Q + (int64_t)(q0 + tok0) * qs + (int64_t)h * G * D),
-                                                      (short)0, (int)min(bytes, (int64_t)0x7fffffff), 0x00020000);
+    // (for the end, in vector registers)
+    int64_t mass_at = kv8_row_at(c, Hkv, max(panel, 0), h, prow);
+    int key_v = wkey, live_v = live, rg_v = rg, kg_v = kg, ctx_v = ctx, rows_v = rows;
+    if constexpr (LIST) asm volatile("" : "+v"(mass_at), "+v"(key_v), "+v"(live_v), "+v"(rg_v), "+v"(kg_v), "+v"(ctx_v), "+v"(rows_v));
+    // Row tiles from the first that sees key0.  A tile's first row is head `rem0` of token tok0;
+    // both go on by a tile's rows, and a row's place in the tile takes one comparison.
+    const int rt_lo = max(0, key0 - ctx) * G / kMassQ, rt_hi = cdiv(rows, kMassQ);
+    const int tok_step = kMassQ / G, rem_step = kMassQ - tok_step * G;
+    int tok0 = rt_lo * kMassQ / G, rem0 = rt_lo * kMassQ - tok0 * G;  // of the tile loaded next
+    int head_of[NL];
+    uint32_t place[NL];
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const uint32_t off = place[j] + rem0 * D * 2 + (head_of[j] + rem0 >= G ? (uint32_t)((int)qs - G * D) * 2 : 0u);
-      buffer_load_lds16(rq, dst + (wave + 8 * j) * 512, off, 0);
+      const int r = (wave + 8 * j) * RPB + lane / DC, t = r / G;
+      head_of[j] = r - t * G;
+      place[j] = (uint32_t)(t * (int)qs + head_of[j] * D + kv_chunk<D>(lane % DC, r) * 8) * 2;
     }
-    tok0 += tok_step;
-    rem0 += rem_step;
-    if (rem0 >= G) {
-      rem0 -= G;
-      ++tok0;
-    }
-  };
-  float acc[16];
+    auto gload = [&](auto buf) {
+      bf16* dst = decltype(buf)::value ? sq1 : sq0;
+      // (rows past the last read as zero)
+      const int64_t bytes = ((int64_t)(n - 1 - tok0) * qs + G * D) * 2;
+      const auto rq = __builtin_amdgcn_make_buffer_rsrc((void*)(Q + (int64_t)(q0 + tok0) * qs + (int64_t)h * G * D),
+                                                        (short)0, (int)min(bytes, (int64_t)0x7fffffff), 0x00020000);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-  const float* lp = lse + (int64_t)h * b.n_tokens * G + (int64_t)q0 * G;
-  auto lse_of = [&](int rt) {
-    const int row = rt * kMassQ + 32 * rg + lr;
-    return row < rows ? lp[row] : INFINITY;
-  };
-  // Both matrix product and exponentials take most of a step: those of the tile before run
-  // under the product of this one.  (rows past the end: 2^-inf)
-  float off_next = lse_of(rt_lo), off_old = INFINITY;
-  f32x16 old = f32x16{0.f};
-  auto weigh = [&](auto e_) {
-    constexpr int e = decltype(e_)::value;
-    acc[e] += __builtin_amdgcn_exp2f(fmaf(old[e], kf, -off_old));
-  };
-  int tok_of = tok0;  // first token of the tile at work
-  gload(Int<0>{});
-  auto step = [&](int rt, auto buf) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      for (int j = 0; j < NL; ++j) {
+        const uint32_t off = place[j] + rem0 * D * 2 + (head_of[j] + rem0 >= G ? (uint32_t)((int)qs - G * D) * 2 : 0u);
+        buffer_load_lds16(rq, dst + (wave + 8 * j) * 512, off, 0);
+      }
+      tok0 += tok_step;
+      rem0 += rem_step;
+      if (rem0 >= G) {
+        rem0 -= G;
+        ++tok0;
+      }
+    };
+    float acc[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    const float* lp = lse + (int64_t)h * b.n_tokens * G + (int64_t)q0 * G;
+    if constexpr (LIST) asm volatile("" : "+v"(lp));
+    auto lse_of = [&](int rt) {
+      const int row = rt * kMassQ + 32 * rg_v + lr;
+      return row < rows_v ? lp[row] : INFINITY;
+    };
+    // Both matrix product and exponentials take most of a step: those of the tile before run
+    // under the product of this one.  (rows past the end: 2^-inf)
+    float off_next = lse_of(rt_lo), off_old = INFINITY;
+    f32x16 old = f32x16{0.f};
+    auto weigh = [&](auto e_) {
+      constexpr int e = decltype(e_)::value;
+      acc[e] += __builtin_amdgcn_exp2f(fmaf(old[e], kf, -off_old));
+    };
+    int tok_of = tok0;  // first token of the tile at work
+    gload(Int<0>{});
+    auto step = [&](int rt, auto buf) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      const float off = off_next;
+      const int first = tok_of;
+      tok_of = tok0;
+      if (rt + 1 < rt_hi) {
+        off_next = lse_of(rt + 1);  // (before the rows: loads come back in order)
+        gload(Int<1 - decltype(buf)::value>{});
+      }
+      const bf16* qb = decltype(buf)::value ? sq1 : sq0;
+      const int r = 32 * rg_v + lr;
+      constexpr int LA = 3;
+      bf16x8 qf[LA + 1];
+      auto qread = [&](int t) { return *(const bf16x8*)&qb[r * D + kv_chunk<D>(2 * t + lg, r) * 8]; };
+#pragma unroll
+      for (int t = 0; t < LA; ++t) qf[t] = qread(t);
+      f32x16 sc = f32x16{0.f};
+      each<DS>([&](auto t_) {
+        constexpr int t = decltype(t_)::value, PER = 16 / DS;
+        if constexpr (t + LA < DS) qf[(t + LA) % (LA + 1)] = qread(t + LA);
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kreg[t], qf[t % (LA + 1)], sc, 0, 0, 0);
+        each<PER>([&](auto j) { weigh(Int<t * PER + decltype(j)::value>{}); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if (key_v + 31 > ctx_v + first) {  // some row may not see some key
+        const int qpos = ctx_v + min(rt * kMassQ + r, rows_v - 1) / G;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (key_v + (e & 3) + 8 * (e >> 2) + 4 * lg > qpos) sc[e] = -INFINITY;
+      }
+      old = sc;
+      off_old = off;
+    };
+    for (int rt = rt_lo; rt < rt_hi; rt += 2) {
+      step(rt, Int<0>{});
+      if (rt + 1 < rt_hi) step(rt + 1, Int<1>{});
+    }
+    each<16>(weigh);
+    // the group's waves: their sums through LDS, added in order
+    float* mp = c.mass + mass_at;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = group_sum(acc[e], 32);
+    if (lr == 0) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sums[rg_v][kg_v][(e & 3) + 8 * (e >> 2) + 4 * lg] = acc[e];
+    }
     __syncthreads();
-    const float off = off_next;
-    const int first = tok_of;
-    tok_of = tok0;
-    if (rt + 1 < rt_hi) {
-      off_next = lse_of(rt + 1);  // (before the rows: loads come back in order)
-      gload(Int<1 - decltype(buf)::value>{});
+    if (rg_v == 0 && lane < live_v) {
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < RG; ++r) sum += sums[r][kg_v][lane];
+      mp[lane] += sum;
     }
-    const bf16* qb = decltype(buf)::value ? sq1 : sq0;
-    const int r = 32 * rg + lr;
-    constexpr int LA = 3;
-    bf16x8 qf[LA + 1];
-    auto qread = [&](int t) { return *(const bf16x8*)&qb[r * D + kv_chunk<D>(2 * t + lg, r) * 8]; };
-#pragma unroll
-    for (int t = 0; t < LA; ++t) qf[t] = qread(t);
-    f32x16 sc = f32x16{0.f};
-    each<DS>([&](auto t_) {
-      constexpr int t = decltype(t_)::value, PER = 16 / DS;
-      if constexpr (t + LA < DS) qf[(t + LA) % (LA + 1)] = qread(t + LA);
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kreg[t], qf[t % (LA + 1)], sc, 0, 0, 0);
-      each<PER>([&](auto j) { weigh(Int<t * PER + decltype(j)::value>{}); });
-      __builtin_amdgcn_sched_barrier(0);
-    });
-    if (wkey + 31 > ctx + first) {  // some row may not see some key
-      const int qpos = ctx + min(rt * kMassQ + r, rows - 1) / G;
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (wkey + (e & 3) + 8 * (e >> 2) + 4 * lg > qpos) sc[e] = -INFINITY;
-    }
-    old = sc;
-    off_old = off;
-  };
-  for (int rt = rt_lo; rt < rt_hi; rt += 2) {
-    step(rt, Int<0>{});
-    if (rt + 1 < rt_hi) step(rt + 1, Int<1>{});
-  }
-  each<16>(weigh);
-  // the group's waves: their sums through LDS, added in order
-  float* mp = c.mass + kv8_row_at(c, Hkv, max(panel, 0), h, prow);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = group_sum(acc[e], 32);
-  if (lr == 0) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sums[rg][kg][(e & 3) + 8 * (e >> 2) + 4 * lg] = acc[e];
-  }
-  __syncthreads();
-  if (rg == 0 && lane < live) {
-    float sum = 0.f;
-#pragma unroll
-    for (int r = 0; r < RG; ++r) sum += sums[r][kg][lane];
-    mp[lane] += sum;
-  }
+    item += gridDim.x;
+  } while (LIST);
 }
 
 // Key-range splits: doubled while the workgroups fit one to a CU and a split keeps 4 tiles of
@@ -626,15 +655,23 @@ static hipError_t run_flash8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hkv
   if (c.mass) {
     // (as many chunks as the longest would make of the tokens)
     const int64_t wgs4 = (int64_t)cdiv(b.max_ctx_len + b.max_q_len, 128) * Hkv * cdiv(b.n_tokens, b.max_q_len);
-    auto weigh = [&](auto kg, auto kernel) {
-      const int keys = 32 * decltype(kg)::value;
-      kernel<<<dim3(cdiv(b.max_ctx_len + b.max_q_len, keys), Hkv, b.n_seqs), 512, 0, s>>>(
-          b, c, Hq, Hkv, (const bf16*)q, qs, lse, least, scale_log2e);
+    auto weigh = [&](auto kg, auto direct, auto listed) {
+      const int rows = b.max_ctx_len + b.max_q_len, pieces = cdiv(rows, 32 * decltype(kg)::value);
+      const int wgs = 4 * cu_count();
+      if ((int64_t)pieces * Hkv * b.n_seqs > 4 * wgs)
+        listed<<<wgs, 512, 0, s>>>(b, c, Hq, Hkv, (const bf16*)q, qs, lse, least, scale_log2e);
+      else
+        direct<<<dim3(pieces, Hkv, b.n_seqs), 512, 0, s>>>(b, c, Hq, Hkv, (const bf16*)q, qs, lse, least,
+                                                           scale_log2e);
       return hipGetLastError();
     };
-    if (wgs4 * 3 >= 2 * cu_count()) e = weigh(Int<4>{}, attn_kv8_mass_kernel<D, FP8, 4>);
-    else if (wgs4 * 3 >= cu_count()) e = weigh(Int<2>{}, attn_kv8_mass_kernel<D, FP8, 2>);
-    else e = weigh(Int<1>{}, attn_kv8_mass_kernel<D, FP8, 1>);
+    const auto two = attn_kv8_mass_kernel<D, FP8, 2, true>;
+    if (wgs4 * 3 >= 2 * cu_count())
+      e = weigh(Int<4>{}, attn_kv8_mass_kernel<D, FP8, 4, false>, attn_kv8_mass_kernel<D, FP8, 4, true>);
+    else if (wgs4 * 3 >= cu_count())
+      e = weigh(Int<2>{}, attn_kv8_mass_kernel<D, FP8, 2, false>, two);
+    else  // (one group of a listed workgroup would spill scalar registers)
+      e = weigh(Int<1>{}, attn_kv8_mass_kernel<D, FP8, 1, false>, two);
   }
   return e;
 }

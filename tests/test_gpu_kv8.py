@@ -406,6 +406,18 @@ def test_cache_past_32_bits(q):
         assert torch.equal(a[-2:, :, :b.shape[2]].view(torch.uint8), b.view(torch.uint8)), name
 
 
+@pytest.mark.parametrize("rows,chunks", [(9000, 20), (5140, 1), (2540, 1)])
+def test_many_sequences_with_few_chunks(rows, chunks):
+    """More pieces of weight sums than the workgroups that go through them (the groups of 128
+    and of 64 rows), all of the sequences' or one chunk's alone."""
+    cfg = config(4, 2, 64)
+    n = 40
+    q = [(60 if chunks == 1 else 2 + i % 3) if i % (n // chunks) == 1 else 1 for i in range(n)]
+    ctx = [rows - 7 * i if q[i] > 1 else 30 * i for i in range(n)]
+    cache = make_cache(cfg, n, rows + 80, "int8", 64, seed=6)
+    run_attention(cfg, cache, (list(range(n))[::-1], ctx, q))
+
+
 def test_memory_of_the_callers_stream():
     """A workspace that the call allocates and drops comes from its own stream's memory: what
     the current stream allocates right after does not reach into it."""
