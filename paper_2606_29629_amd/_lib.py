@@ -460,45 +460,69 @@ class KV8Cache:
     """An 8-bit KV cache (tri_kv8_cache): codes k, v [panels, Hkv, rows, D] (int8, or
     float8_e4m3fn), a float32 scale per head and scale_rows rows, optionally the rows'
     accumulated attention weight and their tokens' positions.  Contiguous (a panel is a slot),
-    or paged with block_table [n_slots, max_seq / rows] and max_seq."""
+    or paged with block_table [n_slots, max_seq / rows] and max_seq.
+
+    The calls work on the tensors that the attributes k, v, k_scale, v_scale, mass, stamp and
+    block_table name: one of them may be replaced by another of its shape and type (mass and
+    stamp by None too, or set where there were none), as `cache.mass = cache.mass * 0.5` does.
+    The other attributes are fixed."""
+
+    _TENSORS = ("k", "v", "k_scale", "v_scale", "mass", "stamp", "block_table")
 
     def __init__(self, k, v, k_scale, v_scale, scale_rows: int, mass=None, stamp=None,
                  block_table=None, max_seq: Optional[int] = None):
         import torch
         formats = {torch.int8: TRI_KV8_INT8, torch.float8_e4m3fn: TRI_KV8_E4M3}
-        if k.dtype not in formats or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape:
+        if k.dtype not in formats or k.dim() != 4:
             raise ValueError("KV8Cache: k and v are int8 or float8_e4m3fn [panels, Hkv, rows, D]")
-        panels, heads, rows = k.shape[:3]
-        per = -(-rows // int(scale_rows))
-        for name, t, shape, dt in (("k_scale", k_scale, (panels, heads, per), torch.float32),
-                                   ("v_scale", v_scale, (panels, heads, per), torch.float32),
-                                   ("mass", mass, (panels, heads, rows), torch.float32),
-                                   ("stamp", stamp, (panels, heads, rows), torch.int32)):
-            if t is None and name in ("mass", "stamp"):
-                continue
-            if t.dtype != dt or tuple(t.shape) != shape:
-                raise ValueError(f"KV8Cache: {name} is {dt} {shape}")
+        panels, heads, rows, d = k.shape
         if block_table is None:
             if max_seq is not None and max_seq > rows:
                 raise ValueError(f"KV8Cache: max_seq {max_seq} of {rows} rows")
-        elif max_seq is None or block_table.dtype != torch.int32 or \
-                block_table.dim() != 2 or block_table.shape[1] * rows != max_seq:
+        elif max_seq is None or block_table.dim() != 2 or block_table.shape[1] * rows != max_seq:
             raise ValueError("KV8Cache: block_table is int32 [n_slots, max_seq / rows]")
-        tensors = (k, v, k_scale, v_scale, mass, stamp, block_table)
-        if not all(t is None or t.is_contiguous() for t in tensors):
-            raise ValueError("KV8Cache: contiguous tensors expected")
-        if any(t is not None and t.device != k.device for t in tensors):
-            raise ValueError("KV8Cache: tensors on one device expected")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.mass, self.stamp, self.block_table = mass, stamp, block_table
-        self.scale_rows, self.head_dim, self.n_kv_heads = int(scale_rows), int(k.shape[3]), int(heads)
         paged = block_table is not None
-        self.n_slots = int(block_table.shape[0]) if paged else int(panels)
-        self.max_seq = int(max_seq) if paged else int(rows)
-        self._struct = KV8CacheStruct(*[_ptr(t) for t in tensors[:6]], self.n_slots, self.max_seq,
-                                      _ptr(block_table), int(rows) if paged else 0,
-                                      int(panels) if paged else 0, formats[k.dtype], self.scale_rows)
-        self._ref = ctypes.byref(self._struct)  # (the tensors of a cache do not change)
+        fixed = dict(scale_rows=int(scale_rows), head_dim=int(d), n_kv_heads=int(heads),
+                     n_slots=int(block_table.shape[0]) if paged else int(panels),
+                     max_seq=int(max_seq) if paged else int(rows))
+        codes, scales = tuple(k.shape), (panels, heads, -(-rows // fixed["scale_rows"]))
+        self.__dict__.update(fixed, _device=k.device, _kind={
+            "k": (codes, k.dtype), "v": (codes, k.dtype), "k_scale": (scales, torch.float32),
+            "v_scale": (scales, torch.float32), "mass": (codes[:3], torch.float32),
+            "stamp": (codes[:3], torch.int32),
+            "block_table": (tuple(block_table.shape), torch.int32) if paged else None})
+        struct = KV8CacheStruct(n_slots=self.n_slots, max_seq=self.max_seq,
+                                block_size=int(rows) if paged else 0, n_blocks=int(panels) if paged else 0,
+                                format=formats[k.dtype], scale_rows=self.scale_rows)
+        self.__dict__.update(_struct=struct, _ref=ctypes.byref(struct))
+        for name, t in zip(self._TENSORS, (k, v, k_scale, v_scale, mass, stamp, block_table)):
+            setattr(self, name, t)
+
+    def __setattr__(self, name, t):
+        if name not in self._TENSORS:
+            raise AttributeError(f"KV8Cache: {name} cannot be set")
+        kind = self._kind[name]
+        if t is None:
+            if kind is not None and name not in ("mass", "stamp"):
+                raise ValueError(f"KV8Cache: {name} is {kind[1]} {kind[0]}")
+        elif kind is None:
+            raise ValueError(f"KV8Cache: {name} of a contiguous cache")
+        else:
+            if (tuple(t.shape), t.dtype) != kind:
+                raise ValueError(f"KV8Cache: {name} is {kind[1]} {kind[0]}")
+            if not t.is_contiguous():
+                raise ValueError("KV8Cache: contiguous tensors expected")
+            if t.device != self._device:
+                raise ValueError("KV8Cache: tensors on one device expected")
+        self.__dict__[name] = t
+        setattr(self._struct, name, _ptr(t))
+
+    def __delattr__(self, name):
+        raise AttributeError(f"KV8Cache: {name} cannot be deleted")
+
+    def __reduce__(self):  # (a copy has a struct of its own)
+        return KV8Cache, (self.k, self.v, self.k_scale, self.v_scale, self.scale_rows, self.mass, self.stamp,
+                          self.block_table, self.max_seq)
 
     @classmethod
     def empty(cls, cfg: LayerConfig, n_slots: int, max_seq: int, format: str = "int8",
