@@ -6,6 +6,7 @@ current HIP stream.  Loading fails loudly if the library has not been built.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional, Sequence
@@ -294,7 +295,8 @@ def kv_struct(cache) -> KVCache:
 def _layer(fn_name, cfg, w, cache, batch, x, out, workspace, route_idx, route_w, stream):
     import torch
     if out is None:
-        out = torch.empty_like(x)
+        with _memory(stream, x.device):
+            out = torch.empty_like(x)
     if isinstance(cache, KV8Cache):
         if (cfg.n_kv_heads, cfg.head_dim) != (cache.n_kv_heads, cache.head_dim):
             raise ValueError(f"{fn_name}: the cache has {cache.n_kv_heads} heads of {cache.head_dim}")
@@ -304,7 +306,7 @@ def _layer(fn_name, cfg, w, cache, batch, x, out, workspace, route_idx, route_w,
         kc = kv_struct(cache)
     need = workspace_size(cfg, batch, cache)
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=x.device)
+        workspace = _empty(stream, max(need, 1), torch.uint8, x.device)
     ws = weights_struct(w)
     b = batch.struct()
     st = getattr(lib(), fn_name)(ctypes.byref(cfg), ctypes.byref(ws), ctypes.byref(kc),
@@ -421,15 +423,22 @@ def _on_gpu(what: str, stream, first, *others) -> Optional[int]:
     return getattr(stream, "cuda_stream", stream)
 
 
-def _empty(stream, shape, dtype, device):
-    """torch.empty from the memory of the stream that the call runs on: what is freed when
-    the call returns is not handed to another stream while the kernels still use it."""
+def _memory(stream, device):
+    """A context in which torch allocates from the memory of the stream that a call runs on:
+    what is freed when the call returns is not handed to another stream while the kernels
+    still use it."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return contextlib.nullcontext()
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(stream, device=device)
-    with torch.cuda.stream(stream):
+    return torch.cuda.stream(stream)
+
+
+def _empty(stream, shape, dtype, device):
+    """torch.empty from the memory of the call's stream."""
+    import torch
+    with _memory(stream, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
