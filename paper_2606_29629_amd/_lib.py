@@ -339,7 +339,8 @@ def layer_decode_noalloc(cfg, w, cache, batch, x, out=None, route_idx=None, rout
     tri_layer_decode_noalloc); returns out."""
     import torch
     if out is None:
-        out = torch.empty_like(x)
+        with _memory(stream, x.device):
+            out = torch.empty_like(x)
     ws = weights_struct(w)
     kc = kv_struct(cache)
     b = batch.struct()
@@ -371,10 +372,10 @@ def linear(a, b, out=None, workspace=None, stream=None):
     M, K = a.shape
     N = b.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=torch.bfloat16, device=a.device)
+        out = _empty(stream, (M, N), torch.bfloat16, a.device)
     need = linear_workspace_size(M, N, K)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=a.device)
+        workspace = _empty(stream, need, torch.uint8, a.device)
     wb = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(lib().tri_linear(_ptr(a), _ptr(b), _ptr(out), M, N, K, _ptr(workspace), wb,
                             _stream(stream)), "tri_linear")
@@ -438,6 +439,8 @@ def _memory(stream, device):
 def _empty(stream, shape, dtype, device):
     """torch.empty from the memory of the call's stream."""
     import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
     with _memory(stream, device):
         return torch.empty(shape, dtype=dtype, device=device)
 

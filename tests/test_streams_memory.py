@@ -55,3 +55,14 @@ def test_layer_calls(made, kind, call):
     made.clear()
     out, ws = call(CFG, {}, cache, batch, x, stream=HANDLE)
     assert made == [(out.nbytes, True), (ws.nbytes, True)] and ws.nbytes == 4096
+
+
+def test_linear_and_the_step_without_a_workspace(made):
+    x = torch.zeros(1, 64, dtype=torch.bfloat16)
+    made.clear()
+    out = T.linear(x, torch.zeros(32, 64, dtype=torch.bfloat16), stream=HANDLE)
+    assert made == [(out.nbytes, True), (4096, True)]
+    cache, batch = caches()["bf16"], T.DeviceBatch([0], [3], [1], device="cpu")
+    made.clear()
+    out = T.layer_decode_noalloc(CFG, {}, cache, batch, x, stream=HANDLE)
+    assert made == [(out.nbytes, True)]
