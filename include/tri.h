@@ -446,7 +446,8 @@ tri_status tri_kv8_select(const tri_layer_config* cfg, const tri_kv8_cache* cach
  * mass, stamp), r < budget.  A scale block into which rows move takes the largest of
  * its rows' scales; codes are shifted to it.  Rows at or past budget are left as they
  * were, and a later append starts at new_len.  `batch` gives n_seqs and slots (as in
- * the select).  An entry below 0 or at or past max_seq is left out; an entry r' != r
+ * the select).  An entry below 0 or at or past max_seq is left out: its row keeps what it
+ * holds, and counts among the block's rows where others move into it.  An entry r' != r
  * must be >= budget.  A page shared between sequences must not be moved into.     */
 tri_status tri_kv8_move(const tri_layer_config* cfg, const tri_kv8_cache* cache,
                         const tri_batch* batch, const int32_t* plan, int32_t budget,

@@ -591,7 +591,7 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(BatchDev b, Kv8Dev c, int
   const bool live = __builtin_amdgcn_ballot_w64(any) != 0;
   const int64_t row0 = kv8_row_at(c, Hkv, max(panel, 0), h, prow);
   const int64_t at = kv8_scale_at(c, Hkv, max(panel, 0), h, prow);
-  int64_t from[RPL];  // row index of the source, -1: leave the row
+  int64_t from[RPL];  // row index of the source, -1: no row
   float now[2], f[2][RPL];  // the block's scales; factor of each row's codes, 1: as they are
   if (live) {
     float scale[2][RPL];
@@ -600,15 +600,15 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(BatchDev b, Kv8Dev c, int
     for (int j = 0; j < RPL; ++j) {
       from[j] = -1;
       scale[0][j] = scale[1][j] = 0.f;
-      if (src[j] >= 0) {
-        int p;
-        const int sp = kv_panel(c.kv, sl, src[j], p);
-        if (sp >= 0) {
-          from[j] = kv8_row_at(c, Hkv, sp, h, p);
-          const int64_t sa = kv8_scale_at(c, Hkv, sp, h, p);
-          scale[0][j] = c.k_scale[sa];
-          scale[1][j] = c.v_scale[sa];
-        }
+      const int r = lane + 64 * j;
+      if (r < R) {
+        int p = 0;
+        const int sp = src[j] >= 0 ? kv_panel(c.kv, sl, src[j], p) : -1;
+        // (a row that is left out stays, under the block's scale as it comes out)
+        from[j] = sp >= 0 ? kv8_row_at(c, Hkv, sp, h, p) : row0 + r;
+        const int64_t sa = sp >= 0 ? kv8_scale_at(c, Hkv, sp, h, p) : at;
+        scale[0][j] = c.k_scale[sa];
+        scale[1][j] = c.v_scale[sa];
       }
       top[0] = max(top[0], __float_as_uint(scale[0][j]) & 0x7fffffffu);
       top[1] = max(top[1], __float_as_uint(scale[1][j]) & 0x7fffffffu);
