@@ -391,8 +391,8 @@ tri_status tri_kv8_append(const tri_layer_config* cfg, const tri_kv8_cache* cach
  * beside them passes 2^8).  Tokens of a skipped sequence (as in the append) are left as
  * they were.
  * workspace: device, 256-byte aligned, of tri_kv8_attention_workspace_size bytes
- * (the cache's and the batch's host fields are read; it never shrinks as max_ctx_len or
- * n_tokens grows).                                                               */
+ * (the cache's and the batch's host fields are read; it never shrinks as n_tokens, n_seqs,
+ * max_ctx_len or max_q_len grows).                                               */
 tri_status tri_kv8_attention_workspace_size(const tri_layer_config* cfg,
                                             const tri_kv8_cache* cache, const tri_batch* batch,
                                             size_t* bytes);

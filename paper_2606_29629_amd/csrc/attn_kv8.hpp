@@ -7,10 +7,11 @@ namespace tri {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 
-// Splits of a batch's rows: how many, rows of each (a multiple of the tile), and a bound
-// on how many that never falls as the rows grow.
+// Splits of a sequence's rows: how many, rows of each (a multiple of the tile); and a bound
+// on those of all sequences that never falls as the rows or the sequences grow.
 struct Kv8Splits {
-  int n, rows, most;
+  int n, rows;
+  int64_t most;
 };
 size_t attn_kv8_decode_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads, int n_kv_heads,
                              int head_dim);

@@ -34,14 +34,18 @@ static int waves_per_cu8(int head_dim) {
 }
 
 // Splits of max_kv rows: as many as make one round of resident waves, none under
-// kMinSplit8 or over kMaxSplit8 rows.
+// kMinSplit8 or over kMaxSplit8 rows.  `most`: a round's room or the sequences in shortest
+// splits, whichever is less, or the sequences in longest splits.  (Not n_seqs times the
+// splits of one: that product falls where the quotient for one sequence steps down.)
 Kv8Splits kv8_splits(int n_seqs, int n_q_heads, int n_kv_heads, int head_dim, int max_kv) {
-  const int64_t waves = (int64_t)n_seqs * n_kv_heads * cdiv(n_q_heads / n_kv_heads, 16);
-  const int64_t resident = (int64_t)waves_per_cu8(head_dim) * cu_count();
-  const int64_t want = std::max<int64_t>(1, resident / std::max<int64_t>(1, waves));
+  const int64_t per_split = (int64_t)n_kv_heads * cdiv(n_q_heads / n_kv_heads, 16);  // waves
+  const int64_t resident = (int64_t)waves_per_cu8(head_dim) * cu_count(), seqs = std::max(n_seqs, 1);
+  const int64_t want = std::max<int64_t>(1, resident / (per_split * seqs));
   const int n = (int)std::min<int64_t>(want, cdiv(max_kv, kMinSplit8));
   const int rows = std::min(cdiv(cdiv(max_kv, n), kTile8) * kTile8, kMaxSplit8);
-  return Kv8Splits{cdiv(max_kv, rows), rows, std::max(n, cdiv(max_kv, kMaxSplit8))};
+  const int64_t most = std::max(std::min(resident / per_split, seqs * cdiv(max_kv, kMinSplit8)),
+                                seqs * cdiv(max_kv, kMaxSplit8));
+  return Kv8Splits{cdiv(max_kv, rows), rows, most};
 }
 
 __device__ __forceinline__ uint32_t lds_offset(const void* p) {
@@ -403,8 +407,8 @@ static size_t score_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads) {
 }
 size_t attn_kv8_decode_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads, int n_kv_heads,
                              int head_dim) {
-  const int most = kv8_splits(b.n_seqs, n_q_heads, n_kv_heads, head_dim, b.max_ctx_len + 1).most;
-  return (size_t)b.n_seqs * n_q_heads * most * (head_dim + 4) * 4 + score_bytes(b, c, n_q_heads);
+  const int64_t most = kv8_splits(b.n_seqs, n_q_heads, n_kv_heads, head_dim, b.max_ctx_len + 1).most;
+  return (size_t)most * n_q_heads * (head_dim + 4) * 4 + score_bytes(b, c, n_q_heads);
 }
 
 template <int D, bool FP8>
@@ -412,7 +416,7 @@ static hipError_t run_decode8(const BatchDev& b, const Kv8Dev& c, int Hq, int Hk
                               int64_t qs, void* out, float* part, hipStream_t s) {
   const int max_kv = b.max_ctx_len + 1;
   const Kv8Splits sp = kv8_splits(b.n_seqs, Hq, Hkv, D, max_kv);
-  float* scores = c.mass ? part + (size_t)b.n_seqs * Hq * sp.most * (D + 4) : nullptr;
+  float* scores = c.mass ? part + (size_t)sp.most * Hq * (D + 4) : nullptr;
   const int ld = cdiv(max_kv, kTile8) * kTile8;
   const float scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
   const dim3 grid(sp.n, Hkv * cdiv(Hq / Hkv, 16), b.n_seqs);
