@@ -193,8 +193,8 @@ typedef struct {
 
 /* Workspace bytes needed by tri_layer_prefill / tri_layer_decode for a batch
  * with these host scalars (device arrays are not read).  For a fixed config the
- * size never decreases as n_tokens grows (other scalars equal), so a workspace
- * sized for the largest batch serves every smaller one.                        */
+ * size never decreases as n_tokens, n_seqs, max_q_len or max_ctx_len grows, so a
+ * workspace sized for the largest batch serves every smaller one.              */
 tri_status tri_workspace_size(const tri_layer_config* cfg, const tri_batch* batch,
                               size_t* bytes);
 
@@ -404,7 +404,7 @@ tri_status tri_kv8_attention(const tri_layer_config* cfg, const tri_kv8_cache* c
  * cache written by tri_kv8_append and attended to by tri_kv8_attention (mass included)
  * in place of the bf16 cache; every other stage is the same.  cfg->dtype is TRI_BF16.
  * The attention sees the step's own rows as the cache holds them.  workspace: of
- * tri_workspace_size_kv8 bytes.                                                   */
+ * tri_workspace_size_kv8 bytes (which never decrease, as those of tri_workspace_size). */
 tri_status tri_workspace_size_kv8(const tri_layer_config* cfg, const tri_kv8_cache* cache,
                                   const tri_batch* batch, size_t* bytes);
 tri_status tri_layer_prefill_kv8(const tri_layer_config* cfg, const tri_layer_weights* w,

@@ -491,8 +491,12 @@ int attn_prefill_splits(int n_seqs, int n_tokens, int max_q_len, int max_ctx_len
 
 size_t attn_prefill_partial_bytes(int n_seqs, int n_tokens, int max_q_len, int max_ctx_len,
                                   int n_q_heads, int head_dim) {
-  const int sp = attn_prefill_splits(n_seqs, n_tokens, max_q_len, max_ctx_len, n_q_heads);
-  return sp > 1 ? (size_t)sp * n_tokens * n_q_heads * (head_dim + 2) * sizeof(float) : 0;
+  // a bound on the splits times the rows that never falls as the batch grows: the splits of
+  // the least batch, or the rows of the 1.25 query tiles per CU that split at most
+  const int most = attn_prefill_splits(1, 1, max_q_len, max_ctx_len, n_q_heads);
+  if (most == 1) return 0;
+  const int64_t rows = std::min((int64_t)most * n_tokens * n_q_heads, (int64_t)cu_count() * 5 / 4 * kFaBQ);
+  return (size_t)rows * (head_dim + 2) * sizeof(float);
 }
 
 template <int D, bool PAGED, bool SPLIT, bool F32 = false>
