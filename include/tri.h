@@ -379,7 +379,7 @@ tri_status tri_kv8_append(const tri_layer_config* cfg, const tri_kv8_cache* cach
  * to rows 0 .. ctx_len[s] + i of its slot, which hold the batch's own rows already
  * (tri_kv8_append first).  Any mix of chunks and single tokens.
  *  q    device bf16 [T][Hq][D], tokens q_stride elements apart (a multiple of 8,
- *       Hq D .. 2^22), 16-byte aligned;  Hq / Hkv <= 32
+ *       Hq D .. 2^22), 16-byte aligned;  Hq / Hkv <= 32, T Hq < 2^31 - 2^23
  *  out  device bf16 [T][Hq][D]; must not overlap q
  * Where the cache has `mass`, mass[row] += the row's attention weights summed over
  * the KV head's query heads and the new tokens of the sequence (in one fixed order:

@@ -68,8 +68,6 @@ tri_status tri::check_batch_scalars(const tri_batch* b) {
 
 namespace {
 
-constexpr int kMaxGridYZ = 65535;  // sequences and heads over an 8-bit cache
-
 // Projections with at most this many rows take the weight-streaming path.
 constexpr int kSkinnyMaxRows = 128;
 
@@ -444,10 +442,13 @@ tri_status tri::layer_call(bool decode, bool timed, const tri_layer_config* cfg,
   if (bias && !w->b_qkv) return TRI_ERR_NULL;
   const bool qk_norm = (cfg->flags & TRI_F_QK_NORM) != 0;
   if (qk_norm && (!w->q_norm || !w->k_norm)) return TRI_ERR_NULL;
-  const int max_seq = cache8 ? cache8->max_seq : cache->max_seq;
-  if (b->max_ctx_len >= max_seq || b->max_q_len > max_seq) return TRI_ERR_RANGE;
-  if (decode && (int64_t)b->max_ctx_len + 1 > max_seq) return TRI_ERR_RANGE;
-  if (cache8 && (b->n_seqs > kMaxGridYZ || cfg->n_q_heads > kMaxGridYZ)) return TRI_ERR_RANGE;
+  if (cache8) {
+    if ((st = check_kv8_batch(cache8, b)) != TRI_OK) return st;
+    if ((st = check_kv8_queries(cfg, b)) != TRI_OK) return st;
+  } else {
+    if (b->max_ctx_len >= cache->max_seq || b->max_q_len > cache->max_seq) return TRI_ERR_RANGE;
+    if (decode && (int64_t)b->max_ctx_len + 1 > cache->max_seq) return TRI_ERR_RANGE;
+  }
   const void* ptrs[] = {x_in, x_out, ws, cache8 ? cache8->k : cache->k,
                         cache8 ? cache8->v : cache->v, w->attn_norm, w->w_qkv, w->w_o,
                         w->mlp_norm, w->w_gate_up, w->w_down};
@@ -708,6 +709,8 @@ tri_status tri_workspace_size_kv8(const tri_layer_config* cfg, const tri_kv8_cac
   if (is_f32(cfg)) return TRI_ERR_UNSUPPORTED;
   if ((st = check_kv8_cache(cache)) != TRI_OK) return st;
   if ((st = check_batch_scalars(batch)) != TRI_OK) return st;
+  if ((st = check_kv8_batch(cache, batch)) != TRI_OK) return st;
+  if ((st = check_kv8_queries(cfg, batch)) != TRI_OK) return st;
   *bytes = layout_of(cfg, batch, cache).total;
   return TRI_OK;
 }

@@ -35,6 +35,12 @@ inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
 
 // The same for an 8-bit cache.
 tri_status check_kv8_cache(const tri_kv8_cache* c);
+// A batch's host scalars against an 8-bit cache that passed, and the attention's query rows.
+tri_status check_kv8_batch(const tri_kv8_cache* c, const tri_batch* b);
+tri_status check_kv8_queries(const tri_layer_config* c, const tri_batch* b);
+// Query rows (tokens times query heads) of a call: 32-bit counts, also with a sequence's most
+// rows added to round them up.
+constexpr int64_t kMaxPackedRows = 0x7fffffff - (1 << 23);
 
 // The layer entry points' common body (tri_layer_prefill when decode is
 // false, tri_layer_decode when true) on a workspace of ws_bytes, over `cache` or, where it is

@@ -44,9 +44,21 @@ Kv8Dev tri::kv8_dev(const tri_kv8_cache* c) {
   return d;
 }
 
-namespace {
-
 constexpr int kMaxGrid = 65535;  // y and z extents of a grid
+
+tri_status tri::check_kv8_batch(const tri_kv8_cache* cache, const tri_batch* b) {
+  if (b->n_seqs > kMaxGrid) return TRI_ERR_RANGE;
+  if (b->max_ctx_len > cache->max_seq || b->max_q_len > cache->max_seq) return TRI_ERR_RANGE;
+  if (b->n_tokens > 0 && b->max_ctx_len >= cache->max_seq) return TRI_ERR_RANGE;
+  return TRI_OK;
+}
+
+tri_status tri::check_kv8_queries(const tri_layer_config* c, const tri_batch* b) {
+  if (c->n_q_heads > kMaxGrid) return TRI_ERR_RANGE;
+  return (int64_t)b->n_tokens * c->n_q_heads > kMaxPackedRows ? TRI_ERR_RANGE : TRI_OK;
+}
+
+namespace {
 
 // The fields of the layer config that these operators read.
 tri_status check_heads(const tri_layer_config* c) {
@@ -71,16 +83,12 @@ tri_status check_call(const tri_layer_config* cfg, const tri_kv8_cache* cache, c
   if ((st = check_batch_scalars(b)) != TRI_OK) return st;
   if (b->n_seqs == 0) return TRI_OK;
   if ((st = check_kv8_cache(cache)) != TRI_OK) return st;
-  if (b->n_seqs > kMaxGrid) return TRI_ERR_RANGE;
-  if (b->max_ctx_len > cache->max_seq || b->max_q_len > cache->max_seq) return TRI_ERR_RANGE;
-  if (b->n_tokens > 0 && b->max_ctx_len >= cache->max_seq) return TRI_ERR_RANGE;
-  return TRI_OK;
+  return check_kv8_batch(cache, b);
 }
 
 tri_status check_group(const tri_layer_config* c) {
   if (c->n_q_heads <= 0 || c->n_q_heads % c->n_kv_heads != 0) return TRI_ERR_SHAPE;
   if (c->n_q_heads / c->n_kv_heads > 32) return TRI_ERR_UNSUPPORTED;
-  if (c->n_q_heads > kMaxGrid) return TRI_ERR_RANGE;
   return TRI_OK;
 }
 
@@ -207,8 +215,8 @@ tri_status tri_kv8_attention_workspace_size(const tri_layer_config* cfg,
   if (!bytes) return TRI_ERR_NULL;
   tri_status st = check_call(cfg, cache, b);
   if (st == TRI_OK) st = check_group(cfg);
+  if (st == TRI_OK) st = check_kv8_queries(cfg, b);
   if (st != TRI_OK) return st;
-  if ((int64_t)b->n_tokens * cfg->n_q_heads > 0x7fffffff) return TRI_ERR_RANGE;
   *bytes = b->n_tokens == 0 ? 0 : attn_kv8_workspace_bytes(batch_dev(b), kv8_dev(cache), cfg->n_q_heads,
                                                            cfg->n_kv_heads, cfg->head_dim);
   return TRI_OK;

@@ -64,3 +64,26 @@ def test_layer_never_shrinks_as_tokens_are_added(lib, layer):  # noqa: F811
                 sizes = [size(lib, c, kv, batch(n_seqs, t, q, ctx))
                          for t in range(max(n_seqs, q), min(n_seqs * q, 3000))]
                 assert sizes == sorted(sizes)
+
+
+def test_layer_checks_the_batch_as_its_attention_does(lib):  # noqa: F811
+    """Host scalars that the attention refuses are refused by the layer's size and calls."""
+    n = ctypes.c_size_t(77)
+    w = T.LayerWeights(*[0x7F0000000000 + (20 << 20) + 4096 * i for i in range(10)])
+    one, many = cfg(), cfg(n_q_heads=64, n_kv_heads=2)
+    for c, kv, b in ((one, cache(), batch(max_ctx=256)), (one, cache(), batch(max_ctx=1 << 30)),
+                     (one, cache(), batch(max_ctx=(1 << 31) - 1)),
+                     (one, cache(), batch(n_seqs=1, n_tokens=257, max_q=257)),
+                     (one, cache(), batch(n_seqs=65536, n_tokens=65536, max_q=4)),
+                     (cfg(n_q_heads=65540, n_kv_heads=65540, head_dim=64), cache(), batch()),
+                     (many, cache(max_seq=4096), batch(n_seqs=60000, n_tokens=60000 * 2000, max_q=2000)),
+                     (cfg(n_q_heads=1, n_kv_heads=1), cache(max_seq=1 << 23),
+                      batch(n_seqs=256, n_tokens=(1 << 31) - 1, max_q=1 << 23))):
+        args = [ctypes.byref(a) for a in (c, kv, b)]
+        assert lib.tri_workspace_size_kv8(*args, ctypes.byref(n)) == T.TRI_ERR_RANGE and n.value == 77
+        assert lib.tri_kv8_attention_workspace_size(*args, ctypes.byref(n)) == T.TRI_ERR_RANGE
+        x = [0x7F0000000000 + (k << 40) for k in (1, 2, 3)]
+        assert lib.tri_layer_prefill_kv8(args[0], ctypes.byref(w), *args[1:], x[0], x[1], None, None, x[2],
+                                         (1 << 64) - 1, None) == T.TRI_ERR_RANGE
+    b = batch(n_tokens=0, max_q=0, max_ctx=256)         # a full cache, nothing new
+    assert lib.tri_workspace_size_kv8(*[ctypes.byref(a) for a in (one, cache(), b)], ctypes.byref(n)) == T.TRI_OK
