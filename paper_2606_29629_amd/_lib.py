@@ -489,8 +489,8 @@ class KV8Cache:
             raise ValueError("KV8Cache: k and v are int8 or float8_e4m3fn [panels, Hkv, rows, D]")
         panels, heads, rows, d = k.shape
         if block_table is None:
-            if max_seq is not None and max_seq > rows:
-                raise ValueError(f"KV8Cache: max_seq {max_seq} of {rows} rows")
+            if max_seq is not None and max_seq != rows:  # (a slot's rows lie max_seq apart)
+                raise ValueError(f"KV8Cache: max_seq {max_seq} of a contiguous cache of {rows} rows")
         elif max_seq is None or block_table.dim() != 2 or block_table.shape[1] * rows != max_seq:
             raise ValueError("KV8Cache: block_table is int32 [n_slots, max_seq / rows]")
         paged = block_table is not None

@@ -78,3 +78,12 @@ def test_a_copy_has_its_own_tensors_and_struct():
         assert shallow.k is cache.k and deep.k.data_ptr() != cache.k.data_ptr()
         for c in (shallow, deep):
             assert addresses(c) == named(c) and c.max_seq == cache.max_seq and c.n_slots == cache.n_slots
+
+
+def test_max_seq_of_a_contiguous_cache_is_its_rows():
+    c = make()
+    args = c.k, c.v, c.k_scale, c.v_scale, 32
+    for n in (32, 63, 65, 0):
+        with pytest.raises(ValueError, match="max_seq"):
+            T.KV8Cache(*args, max_seq=n)
+    assert T.KV8Cache(*args, max_seq=64).max_seq == T.KV8Cache(*args).max_seq == 64
