@@ -400,12 +400,12 @@ def make_rope(head_dim: int, rotary_dim: Optional[int] = None, base: float = 1e6
 
 
 def _rows(x, what: str, last: int) -> int:
-    """Token stride of x [tokens, heads, last] whose heads are contiguous."""
+    """Token stride of x [tokens, heads, last] whose heads are contiguous (of one token: any)."""
     if x.dim() == 3:
         n, heads, d = x.shape
         st = x.stride()
         if d == last and st[2] == 1 and (heads <= 1 or st[1] == last):
-            return st[0] if n > 1 else max(st[0], heads * last)
+            return st[0] if n > 1 else heads * last
     raise ValueError(f"{what}: [tokens, heads, {last}] with contiguous heads expected")
 
 

@@ -87,3 +87,26 @@ def test_max_seq_of_a_contiguous_cache_is_its_rows():
         with pytest.raises(ValueError, match="max_seq"):
             T.KV8Cache(*args, max_seq=n)
     assert T.KV8Cache(*args, max_seq=64).max_seq == T.KV8Cache(*args).max_seq == 64
+
+
+def test_one_token_of_rows_of_any_stride(monkeypatch):
+    """Strides that no token follows are not looked at: a key beside a value of other rows, rows
+    of an odd width."""
+    import types
+    table, asked = T.make_rope(64), []
+    call = lambda *a: asked.append(a) or 0
+    monkeypatch.setattr(T, "lib", lambda: types.SimpleNamespace(tri_kv8_append=call, tri_kv8_attention=call, tri_rope=call))
+    monkeypatch.setattr(T, "_on_gpu", lambda what, stream, *tensors: 0)
+    monkeypatch.setattr(T, "kv8_attention_workspace_size", lambda *a: 256)
+    cache, b = make(), T.DeviceBatch([1], [5], [1], device="cpu")
+    cfg = T.LayerConfig(n_q_heads=4, n_kv_heads=2, head_dim=64)
+    row = torch.zeros(1, 1003, dtype=torch.bfloat16)
+    heads = lambda first, n: row.as_strided((1, n, 64), (1003, 64, 1), first)
+    k = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    T.kv8_append(cfg, cache, b, k, heads(128, 2))
+    T.kv8_attention(cfg, cache, b, heads(0, 4))
+    T.rope(table, heads(0, 4), torch.zeros(1, dtype=torch.int32), out=torch.zeros(1, 4, 64, dtype=torch.bfloat16))
+    assert asked[0][5] == 128 and asked[1][4] == 256 and asked[2][2] == asked[2][4] == 256
+    b2, k2 = T.DeviceBatch([1], [5], [2], device="cpu"), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="one token stride"):
+        T.kv8_append(cfg, cache, b2, k2, torch.zeros(2, 4, 64, dtype=torch.bfloat16)[:, :2])
