@@ -533,7 +533,7 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
     auto step = [&](int rt, auto buf) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
-      const float off = off_next;
+      float off = off_next;
       const int first = tok_of;
       tok_of = tok0;
       if (rt + 1 < rt_hi) {
@@ -557,9 +557,12 @@ __global__ __launch_bounds__(512, 2) void attn_kv8_mass_kernel(BatchDev b, Kv8De
       });
       if (key_v + 31 > ctx_v + first) {  // some row may not see some key
         const int qpos = ctx_v + min(rt * kMassQ + r, rows_v - 1) / G;
+        // (a row without finite weights, lse NaN or -inf: NaN to what it sees, 0 to the rest)
+        const bool bad = !(off > -INFINITY);
+        off = bad ? 0.f : off;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (key_v + (e & 3) + 8 * (e >> 2) + 4 * lg > qpos) sc[e] = -INFINITY;
+          sc[e] = key_v + (e & 3) + 8 * (e >> 2) + 4 * lg > qpos ? -INFINITY : (bad ? __builtin_nanf("") : sc[e]);
       }
       old = sc;
       off_old = off;
