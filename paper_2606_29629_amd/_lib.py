@@ -410,8 +410,8 @@ def _rows(x, what: str, last: int) -> int:
 
 
 def _on_gpu(what: str, stream, first, *others) -> Optional[int]:
-    """The kernels follow plain addresses: every tensor of a call on the current GPU.
-    Returns the handle of `stream`, or of the current stream."""
+    """The kernels follow plain addresses: every tensor of a call on the current GPU, and the
+    stream too.  Returns the handle of `stream`, or of the current stream."""
     import torch
     dev = first.get_device()
     for t in others:
@@ -421,6 +421,8 @@ def _on_gpu(what: str, stream, first, *others) -> Optional[int]:
         raise ValueError(f"{what}: tensors on {first.device}, not on the current GPU")
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(dev)
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError(f"{what}: tensors on {first.device}, a stream of GPU {stream.device_index}")
     return getattr(stream, "cuda_stream", stream)
 
 

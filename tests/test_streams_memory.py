@@ -66,3 +66,13 @@ def test_linear_and_the_step_without_a_workspace(made):
     made.clear()
     out = T.layer_decode_noalloc(CFG, {}, cache, batch, x, stream=HANDLE)
     assert made == [(out.nbytes, True)]
+
+
+def test_a_stream_of_another_gpu_is_refused(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    tensor = types.SimpleNamespace(get_device=lambda: 0, device="cuda:0")
+    stream = types.SimpleNamespace(cuda_stream=HANDLE, device_index=0)
+    assert T._on_gpu("call", stream, tensor, None, tensor) == T._on_gpu("call", HANDLE, tensor) == HANDLE
+    stream.device_index = 1
+    with pytest.raises(ValueError, match="stream of GPU 1"):
+        T._on_gpu("call", stream, tensor, tensor)
