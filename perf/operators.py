@@ -151,6 +151,12 @@ def _seqs(case):
 
 # --------------------------------------------------------------- the inputs --
 
+def _max_seq(case, seqs):
+    """Rows of a sequence's slot: its longest, and an eviction's budget (which a sequence may
+    lie below), in whole pages."""
+    return -(-max(case.get("budget", 0), *(q + c for q, c in seqs)) // BLOCK) * BLOCK
+
+
 def _inputs(case, seed):
     """Everything a pass reads, from the seed alone."""
     L = LAYERS[case["layer"]]
@@ -174,7 +180,7 @@ def _inputs(case, seed):
 
     seqs, R = _seqs(case), case["scale_rows"]
     n, T = len(seqs), sum(q for q, _ in seqs)
-    max_seq = -(-max(q + c for q, c in seqs) // BLOCK) * BLOCK
+    max_seq = _max_seq(case, seqs)
     slots = [(i * 5 + 2) % n if n % 5 else (i + 2) % n for i in range(n)]  # a fixed permutation
     table, panels, rows = None, n, max_seq
     if case["paged"]:
