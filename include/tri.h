@@ -384,8 +384,10 @@ tri_status tri_kv8_append(const tri_layer_config* cfg, const tri_kv8_cache* cach
  * Where the cache has `mass`, mass[row] += the row's attention weights summed over
  * the KV head's query heads and the new tokens of the sequence (in one fixed order:
  * the same inputs give the same sums).  Codes are exact in the products; scores,
- * running maximum, sums and outputs are float32, attention weights rounded to 11 bits
- * for the product with the values.  A weight counts in its output's denominator down
+ * running maximum, sums and outputs are float32.  For the product with the values a
+ * weight times its value's scale is rounded to 11 bits, or, where it is below 2^-14 of
+ * the token's largest such product, to a multiple of at most 2^-24 of that: a channel that
+ * only rows of far smaller value scales fill has as many bits fewer.  A weight counts in its output's denominator down
  * to 2^(d - 126) of the largest, where the value scales of the rows that the token sees
  * differ by up to 2^d (zeros have the scale 2^-100: d < 102, so 2^-24, while no value
  * beside them passes 2^8).  Tokens of a skipped sequence (as in the append) are left as
@@ -403,6 +405,9 @@ tri_status tri_kv8_attention(const tri_layer_config* cfg, const tri_kv8_cache* c
 /* The decoder layer over an 8-bit cache: tri_layer_prefill and tri_layer_decode with the
  * cache written by tri_kv8_append and attended to by tri_kv8_attention (mass included)
  * in place of the bf16 cache; every other stage is the same.  cfg->dtype is TRI_BF16.
+ * The per-stage timers count the append as kv_append and all kernels of the attention,
+ * weight sums included, as attn_decode (tri_layer_decode_kv8) or attn_prefill;
+ * tri_layer_work describes the layer on the bf16 cache, with its bytes, alone.
  * The attention sees the step's own rows as the cache holds them.  workspace: of
  * tri_workspace_size_kv8 bytes (which never decrease, as those of tri_workspace_size). */
 tri_status tri_workspace_size_kv8(const tri_layer_config* cfg, const tri_kv8_cache* cache,

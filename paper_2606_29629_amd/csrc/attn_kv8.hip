@@ -615,7 +615,8 @@ static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 static size_t lse_bytes(const BatchDev& b, const Kv8Dev& c, int n_q_heads) {
   return c.mass && b.max_q_len > 1 ? round256((size_t)b.n_tokens * n_q_heads * 4) : 0;
 }
-// (a bound that never falls as tokens are added: splits > 1 leave room for 1.25 CUs' rows)
+// (a bound that never falls as tokens are added: splits > 1 are at most two workgroups' rows
+// per CU)
 static size_t part8_bytes(const BatchDev& b, int n_q_heads, int n_kv_heads, int head_dim) {
   if (b.max_q_len < 2) return 0;
   const int64_t rows = std::min<int64_t>((int64_t)kMaxSplitF8 * b.n_tokens * n_q_heads,
