@@ -479,7 +479,7 @@ class KV8Cache:
     The calls work on the tensors that the attributes k, v, k_scale, v_scale, mass, stamp and
     block_table name: one of them may be replaced by another of its shape and type (mass and
     stamp by None too, or set where there were none), as `cache.mass = cache.mass * 0.5` does.
-    The other attributes are fixed."""
+    (A captured graph keeps those it was captured with.)  The other attributes are fixed."""
 
     _TENSORS = ("k", "v", "k_scale", "v_scale", "mass", "stamp", "block_table")
 
