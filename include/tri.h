@@ -386,12 +386,12 @@ tri_status tri_kv8_append(const tri_layer_config* cfg, const tri_kv8_cache* cach
  * the same inputs give the same sums).  Codes are exact in the products; scores,
  * running maximum, sums and outputs are float32.  For the product with the values a
  * weight times its value's scale is rounded to 11 bits, or, where it is below 2^-14 of
- * the token's largest such product, to a multiple of at most 2^-24 of that: a channel that
- * only rows of far smaller value scales fill has as many bits fewer.  A weight counts in its output's denominator down
- * to 2^(d - 126) of the largest, where the value scales of the rows that the token sees
- * differ by up to 2^d (zeros have the scale 2^-100: d < 102, so 2^-24, while no value
- * beside them passes 2^8).  Tokens of a skipped sequence (as in the append) are left as
- * they were.
+ * the token's largest such product, to a multiple of at most 2^-24 of that: a channel
+ * that only rows of far smaller value scales fill has as many bits fewer.  A weight
+ * counts in its output's denominator down to 2^(d - 126) of the largest, where the value
+ * scales of the rows that the token sees differ by up to 2^d (zeros have the scale
+ * 2^-100: d < 102, so 2^-24, while no value beside them passes 2^8).  Tokens of a skipped
+ * sequence (as in the append) are left as they were.
  * workspace: device, 256-byte aligned, of tri_kv8_attention_workspace_size bytes
  * (the cache's and the batch's host fields are read; it never shrinks as n_tokens, n_seqs,
  * max_ctx_len or max_q_len grows).                                               */
